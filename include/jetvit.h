@@ -261,6 +261,33 @@ jv_status jv_out_proj(const void* o, const void* w, const float* bias, void* y, 
                       void* cuda_stream);
 
 /*
+ * Layer norm of token rows, the normalisation that the blocks of the base models (Sec. 4.1) have in front of every projection,
+ * and its gradient.
+ *   y[r, c]  = (x[r, c] - mean_r) * rstd_r * w[c] + b[c],   rstd_r = 1 / sqrt(var_r + eps), var_r = mean_c (x - mean_r)^2
+ *   dx = rstd (g - mean_c(g) - xh mean_c(g xh)),  g = dy w,  xh = (x - mean) rstd;   dw = sum_r dy xh,  db = sum_r dy
+ * x and dy are [rows, C] arrays of shape.dtype whose rows start x_stride / dy_stride elements apart (0: C, else >= C); y and
+ * dx are [rows, C] contiguous, of the same type.  w, b, dw, db are fp32 [C], mean and rstd fp32 [rows].  w NULL: 1; b NULL: 0.
+ * The forward pass writes mean and rstd if they are not NULL (both or neither); the gradient reads them.  dw or db NULL: not
+ * wanted; with both NULL no scratch is needed.
+ * rows > 0, 0 < C <= 16384, eps >= 0.  Any alignment to the element is served; where every row and vector starts on a 16-byte boundary,
+ * 16 bytes at a time.  Outputs share no byte with an input or each other.  Arithmetic in fp32, statistics of the centred
+ * values; dw and db are summed in a fixed order (results repeat bit for bit).
+ * jv_layer_norm_grad_workspace_bytes() sizes ws (256-byte aligned); 0 on invalid arguments.
+ */
+typedef struct {
+  int64_t rows;
+  int32_t C;
+  int32_t dtype;       /* jv_dtype of x, dy, y, dx */
+  int64_t x_stride;    /* elements from row to row of x; 0 = C */
+  int64_t dy_stride;   /* of dy (gradient only); 0 = C */
+} jv_norm_shape;
+jv_status jv_layer_norm(const void* x, const float* w, const float* b, void* y, float* mean, float* rstd,
+                        const jv_norm_shape* shape, float eps, void* cuda_stream);
+size_t jv_layer_norm_grad_workspace_bytes(const jv_norm_shape* shape);
+jv_status jv_layer_norm_grad(const void* dy, const void* x, const float* w, const float* mean, const float* rstd, void* dx,
+                             float* dw, float* db, const jv_norm_shape* shape, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/*
  * Synchronises the stream, then returns and clears the sticky device status:
  * JV_OK, JV_ERR_TIMEOUT if a kernel abandoned a bounded wait since the last
  * call, or JV_ERR_CUDA if the stream reports a CUDA error.

@@ -120,6 +120,35 @@ jv_status from_cuda(cudaError_t e) {
   return JV_ERR_CUDA;
 }
 
+// A stretch of memory that a call reads or writes
+struct Span {
+  const void* p;
+  size_t bytes;
+};
+// every output against every input and the outputs before it; null pointers take no part
+bool outputs_clash(const Span* in, int nin, const Span* out, int nout) {
+  for (int i = 0; i < nout; ++i) {
+    if (!out[i].p) continue;
+    for (int j = 0; j < nin; ++j)
+      if (in[j].p && overlaps(out[i].p, out[i].bytes, in[j].p, in[j].bytes)) return true;
+    for (int j = 0; j < i; ++j)
+      if (out[j].p && overlaps(out[i].p, out[i].bytes, out[j].p, out[j].bytes)) return true;
+  }
+  return false;
+}
+
+jv_status check_norm(const jv_norm_shape* s) {
+  if (!s || s->rows <= 0 || s->C <= 0) return JV_ERR_INVALID_ARG;
+  if (s->dtype != JV_F32 && s->dtype != JV_BF16) return JV_ERR_INVALID_ARG;
+  if (s->C > 16384 || s->rows > 0x7fffffffll) return JV_ERR_UNSUPPORTED;
+  if ((s->x_stride != 0 && s->x_stride < s->C) || (s->dy_stride != 0 && s->dy_stride < s->C)) return JV_ERR_INVALID_ARG;
+  if (s->x_stride > ((int64_t)1 << 31) || s->dy_stride > ((int64_t)1 << 31)) return JV_ERR_UNSUPPORTED;
+  return JV_OK;
+}
+size_t norm_rows_bytes(const jv_norm_shape* s, int64_t stride) {
+  return (size_t)((s->rows - 1) * (stride ? stride : s->C) + s->C) * (s->dtype == JV_F32 ? 4 : 2);
+}
+
 float pick_scale(float scale, int D) { return scale > 0.f ? scale : 1.f / sqrtf((float)D); }
 
 // ---- enqueue helpers (arguments already validated) ---------------------------
@@ -382,6 +411,48 @@ jv_status jv_out_proj(const void* o, const void* w, const float* bias, void* y, 
   int* status = device_status_ptr();
   if (!status) return JV_ERR_CUDA;
   return from_cuda(launch_proj_tc(false, o, w, bias, y, nullptr, nullptr, *shape, status, (cudaStream_t)cuda_stream));
+}
+
+jv_status jv_layer_norm(const void* x, const float* w, const float* b, void* y, float* mean, float* rstd,
+                        const jv_norm_shape* shape, float eps, void* cuda_stream) {
+  jv_status st = check_norm(shape);
+  if (st != JV_OK) return st;
+  const size_t e = shape->dtype == JV_F32 ? 4 : 2;
+  if (!x || !y || (!mean != !rstd) || !(eps >= 0.f)) return JV_ERR_INVALID_ARG;
+  if (!aligned(x, e) || !aligned(y, e) || !aligned(w, 4) || !aligned(b, 4) || !aligned(mean, 4) || !aligned(rstd, 4)) return JV_ERR_INVALID_ARG;
+  const size_t vec = (size_t)shape->C * 4, per_row = (size_t)shape->rows * 4;
+  const Span in[3] = {{x, norm_rows_bytes(shape, shape->x_stride)}, {w, vec}, {b, vec}};
+  const Span out[3] = {{y, norm_rows_bytes(shape, 0)}, {mean, per_row}, {rstd, per_row}};
+  if (outputs_clash(in, 3, out, 3)) return JV_ERR_INVALID_ARG;
+  if ((st = check_device()) != JV_OK) return st;
+  const NormArgs a{x, nullptr, w, b, y, mean, rstd, shape->rows, shape->x_stride ? shape->x_stride : shape->C, 0, shape->C, shape->dtype, eps};
+  return from_cuda(launch_layer_norm(a, (cudaStream_t)cuda_stream));
+}
+
+size_t jv_layer_norm_grad_workspace_bytes(const jv_norm_shape* shape) {
+  if (check_norm(shape) != JV_OK) return 0;
+  return (size_t)layer_norm_grad_blocks(shape->rows, shape->C) * 2 * shape->C * 4;
+}
+
+jv_status jv_layer_norm_grad(const void* dy, const void* x, const float* w, const float* mean, const float* rstd, void* dx,
+                             float* dw, float* db, const jv_norm_shape* shape, void* ws, size_t ws_bytes, void* cuda_stream) {
+  jv_status st = check_norm(shape);
+  if (st != JV_OK) return st;
+  const size_t e = shape->dtype == JV_F32 ? 4 : 2;
+  if (!dy || !x || !mean || !rstd || !dx) return JV_ERR_INVALID_ARG;
+  if (!aligned(dy, e) || !aligned(x, e) || !aligned(dx, e) || !aligned(w, 4) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dw, 4) ||
+      !aligned(db, 4))
+    return JV_ERR_INVALID_ARG;
+  const size_t vec = (size_t)shape->C * 4, per_row = (size_t)shape->rows * 4;
+  const size_t need = dw || db ? jv_layer_norm_grad_workspace_bytes(shape) : 0;
+  const Span in[5] = {{dy, norm_rows_bytes(shape, shape->dy_stride)}, {x, norm_rows_bytes(shape, shape->x_stride)}, {w, vec}, {mean, per_row}, {rstd, per_row}};
+  const Span out[4] = {{dx, norm_rows_bytes(shape, 0)}, {dw, vec}, {db, vec}, {need ? ws : nullptr, need}};
+  if (outputs_clash(in, 5, out, 4)) return JV_ERR_INVALID_ARG;
+  if ((st = check_ws(ws, ws_bytes, need)) != JV_OK) return st;
+  if ((st = check_device()) != JV_OK) return st;
+  const NormArgs a{x, dy, w, nullptr, dx, const_cast<float*>(mean), const_cast<float*>(rstd), shape->rows,
+                   shape->x_stride ? shape->x_stride : shape->C, shape->dy_stride ? shape->dy_stride : shape->C, shape->C, shape->dtype, 0.f};
+  return from_cuda(launch_layer_norm_grad(a, (float*)ws, dw, db, (cudaStream_t)cuda_stream));
 }
 
 jv_status jv_device_status(void* cuda_stream) {

@@ -253,4 +253,18 @@ bool proj_tc_available();
 cudaError_t launch_proj_tc(bool qkv, const void* x, const void* w, const float* bias, void* d0, void* d1, void* d2,
                            const jv_shape& s, int* status, cudaStream_t st);
 
+// Layer norm of token rows and its gradient
+struct NormArgs {
+  const void *x, *dy;        // dy: gradient only
+  const float *w, *b;
+  void* y;                   // y, or dx
+  float *mean, *rstd;        // forward: outputs or null; gradient: inputs
+  int64_t rows, x_stride, dy_stride;
+  int C, dtype;
+  float eps;
+};
+cudaError_t launch_layer_norm(const NormArgs& a, cudaStream_t st);
+int layer_norm_grad_blocks(int64_t rows, int C);   // partial: [this many, 2, C]
+cudaError_t launch_layer_norm_grad(const NormArgs& a, float* partial, float* dw, float* db, cudaStream_t st);
+
 }  // namespace jv

@@ -1,0 +1,356 @@
+// Layer norm of token rows and its gradient, in front of the projections of a block.
+//
+//   y = (x - m) r w + b,  m = mean x,  r = 1 / sqrt(mean (x - m)^2 + eps)             per row of C values
+//   g = dy w,  xh = (x - m) r:   dx = r (g - mean g - xh mean(g xh)),  dw = sum_rows dy xh,  db = sum_rows dy
+//
+// Both are bound by HBM: a row is read once, held in registers, and written once.  A row of up to 1024 values belongs to a warp
+// (up to 32 values a lane, in 16-byte pieces 32 lanes side by side), a longer one to a block; sums are fp32, the variance is
+// that of the centred values (no cancellation where a row's mean is large against its spread).
+//
+// The gradient's blocks are persistent: every lane keeps the sums of its columns for dw and db in registers over the rows that its
+// warp walks, the warps of a block add theirs through shared memory, the blocks' partials go to the workspace and a second
+// launch adds them up, all in a fixed order: no atomics, results repeat bit for bit.
+#include "common.cuh"
+
+namespace jv {
+namespace {
+
+template <typename T, int VEC>
+struct Piece;                       // VEC consecutive values as they lie in memory
+template <>
+struct Piece<__nv_bfloat16, 8> {
+  uint4 r;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { r = __ldcs(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    const uint32_t u[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(u[i] << 16);
+      f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+  }
+  __device__ __forceinline__ void set(const float (&f)[8]) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 t = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+      u[i] = *reinterpret_cast<const uint32_t*>(&t);
+    }
+    r = make_uint4(u[0], u[1], u[2], u[3]);
+  }
+  __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint4*>(p) = r; }
+};
+template <>
+struct Piece<float, 4> {
+  float4 r;
+  __device__ __forceinline__ void load(const float* p) { r = __ldcs(reinterpret_cast<const float4*>(p)); }
+  __device__ __forceinline__ void get(float (&f)[4]) const { f[0] = r.x; f[1] = r.y; f[2] = r.z; f[3] = r.w; }
+  __device__ __forceinline__ void set(const float (&f)[4]) { r = make_float4(f[0], f[1], f[2], f[3]); }
+  __device__ __forceinline__ void store(float* p) const { *reinterpret_cast<float4*>(p) = r; }
+};
+template <typename T>
+struct Piece<T, 1> {
+  T r;
+  __device__ __forceinline__ void load(const T* p) { r = __ldcs(p); }
+  __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = to_f32(r); }
+  __device__ __forceinline__ void set(const float (&f)[1]) { from_f32(&r, f[0]); }
+  __device__ __forceinline__ void store(T* p) const { *p = r; }
+};
+
+// VEC fp32 values: weights and biases, partial sums
+template <int VEC>
+__device__ __forceinline__ void load_f32(const float* p, float (&f)[VEC]) {
+  if constexpr (VEC == 1) {
+    f[0] = __ldg(p);
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; i += 4) {
+      const float4 v = __ldg(reinterpret_cast<const float4*>(p + i));
+      f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w;
+    }
+  }
+}
+
+// Sums over the threads that share a row: a warp, or the block (red: 2 x 32 floats of shared memory, used in turn)
+template <bool BLOCK, int N>
+__device__ __forceinline__ void row_sums(float (&s)[N], float* red, int& turn) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) s[i] = warp_sum(s[i]);
+  if (!BLOCK) return;
+  const int warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
+  float* dst = red + turn * 32 * N;                 // the other half: the one before may still be read
+  turn ^= 1;
+  if ((threadIdx.x & 31) == 0)
+#pragma unroll
+    for (int i = 0; i < N; ++i) dst[N * warp + i] = s[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    s[i] = 0.f;
+    for (int w = 0; w < nwarps; ++w) s[i] += dst[N * w + i];
+  }
+}
+
+struct NormParams {
+  const void *x, *dy;
+  const float *w, *b;
+  void* y;                          // y, or dx
+  float *mean, *rstd;               // written by the forward pass unless null, read by the gradient
+  float* partial;                   // gradient: [blocks, 2, C]
+  int64_t rows, x_stride, dy_stride;
+  int C;
+  float eps;
+};
+
+// Columns of lane `tl` (of `nl` that share a row): pieces tl, tl + nl, ...
+template <typename T, int VEC, int NCH, bool BLOCK>
+__global__ void __launch_bounds__(BLOCK ? 512 : 128, 1) layer_norm_kernel(const NormParams p) {
+  __shared__ float red[64];
+  griddep_wait();
+  griddep_launch_dependents();
+  const int tl = BLOCK ? threadIdx.x : threadIdx.x & 31, nl = BLOCK ? blockDim.x : 32;
+  const int64_t row = BLOCK ? blockIdx.x : (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  if (row >= p.rows) return;        // (whole warps or blocks)
+  const T* x = (const T*)p.x + row * p.x_stride;
+  Piece<T, VEC> in[NCH];
+#pragma unroll
+  for (int j = 0; j < NCH; ++j) {
+    const int c = (j * nl + tl) * VEC;
+    if (c < p.C) in[j].load(x + c);
+  }
+  const float inv_c = 1.f / (float)p.C;
+  int turn = 0;
+  float s[1] = {0.f};
+#pragma unroll
+  for (int j = 0; j < NCH; ++j)
+    if ((j * nl + tl) * VEC < p.C) {
+      float f[VEC];
+      in[j].get(f);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) s[0] += f[i];
+    }
+  row_sums<BLOCK, 1>(s, red, turn);
+  const float mean = s[0] * inv_c;
+  s[0] = 0.f;
+#pragma unroll
+  for (int j = 0; j < NCH; ++j)
+    if ((j * nl + tl) * VEC < p.C) {
+      float f[VEC];
+      in[j].get(f);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) s[0] = fmaf(f[i] - mean, f[i] - mean, s[0]);
+    }
+  row_sums<BLOCK, 1>(s, red, turn);
+  const float rstd = rsqrtf(fmaf(s[0], inv_c, p.eps));
+  T* y = (T*)p.y + row * p.C;
+#pragma unroll
+  for (int j = 0; j < NCH; ++j) {
+    const int c = (j * nl + tl) * VEC;
+    if (c < p.C) {
+      float f[VEC], w[VEC], b[VEC];
+      in[j].get(f);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) { w[i] = 1.f; b[i] = 0.f; }
+      if (p.w) load_f32<VEC>(p.w + c, w);
+      if (p.b) load_f32<VEC>(p.b + c, b);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) f[i] = fmaf((f[i] - mean) * rstd, w[i], b[i]);
+      in[j].set(f);
+      in[j].store(y + c);
+    }
+  }
+  if (p.mean && tl == 0) {
+    p.mean[row] = mean;
+    p.rstd[row] = rstd;
+  }
+}
+
+// Shared memory: BLOCK: 128 floats; else the block's sums, 2 C floats, added to by its warps one after the other
+template <typename T, int VEC, int NCH, bool BLOCK>
+__global__ void __launch_bounds__(BLOCK ? 512 : 128, 1) layer_norm_grad_kernel(const NormParams p) {
+  extern __shared__ float sm[];
+  griddep_wait();
+  griddep_launch_dependents();
+  const int tl = BLOCK ? threadIdx.x : threadIdx.x & 31, nl = BLOCK ? blockDim.x : 32;
+  const int warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
+  const int64_t first = BLOCK ? blockIdx.x : (int64_t)blockIdx.x * nwarps + warp;
+  const int64_t step = BLOCK ? gridDim.x : (int64_t)gridDim.x * nwarps;
+  float dw[NCH][VEC], db[NCH][VEC];
+#pragma unroll
+  for (int j = 0; j < NCH; ++j)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) dw[j][i] = db[j][i] = 0.f;
+  const float inv_c = 1.f / (float)p.C;
+  int turn = 0;
+  for (int64_t row = first; row < p.rows; row += step) {
+    const T *x = (const T*)p.x + row * p.x_stride, *dy = (const T*)p.dy + row * p.dy_stride;
+    Piece<T, VEC> px[NCH], pd[NCH];
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+      const int c = (j * nl + tl) * VEC;
+      if (c < p.C) {
+        px[j].load(x + c);
+        pd[j].load(dy + c);
+      }
+    }
+    const float mean = __ldg(p.mean + row), rstd = __ldg(p.rstd + row);
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+      const int c = (j * nl + tl) * VEC;
+      if (c < p.C) {
+        float f[VEC], d[VEC], w[VEC];
+        px[j].get(f);
+        pd[j].get(d);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) w[i] = 1.f;
+        if (p.w) load_f32<VEC>(p.w + c, w);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const float xh = (f[i] - mean) * rstd, g = d[i] * w[i];
+          dw[j][i] = fmaf(d[i], xh, dw[j][i]);
+          db[j][i] += d[i];
+          s[0] += g;
+          s[1] = fmaf(g, xh, s[1]);
+        }
+      }
+    }
+    row_sums<BLOCK, 2>(s, sm, turn);
+    const float mg = s[0] * inv_c, mgx = s[1] * inv_c;
+    T* dx = (T*)p.y + row * p.C;
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+      const int c = (j * nl + tl) * VEC;
+      if (c < p.C) {
+        float f[VEC], d[VEC], w[VEC];
+        px[j].get(f);
+        pd[j].get(d);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) w[i] = 1.f;
+        if (p.w) load_f32<VEC>(p.w + c, w);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) f[i] = rstd * (d[i] * w[i] - mg - (f[i] - mean) * rstd * mgx);
+        px[j].set(f);
+        px[j].store(dx + c);
+      }
+    }
+  }
+  if (!p.partial) return;
+  float* part = p.partial + (size_t)blockIdx.x * 2 * p.C;
+  if (BLOCK) {
+#pragma unroll
+    for (int j = 0; j < NCH; ++j)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const int c = (j * nl + tl) * VEC + i;
+        if (c < p.C) {
+          part[c] = dw[j][i];
+          part[p.C + c] = db[j][i];
+        }
+      }
+  } else {
+    for (int w = 0; w < nwarps; ++w) {
+      if (w == warp)
+#pragma unroll
+        for (int j = 0; j < NCH; ++j)
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            const int c = (j * nl + tl) * VEC + i;
+            if (c < p.C) {
+              sm[c] = (w ? sm[c] : 0.f) + dw[j][i];
+              sm[p.C + c] = (w ? sm[p.C + c] : 0.f) + db[j][i];
+            }
+          }
+      __syncthreads();
+    }
+    for (int c = threadIdx.x; c < 2 * p.C; c += blockDim.x) part[c] = sm[c];
+  }
+}
+
+// Column sums of the blocks' partials [n, 2, C]: 32 columns a block, eight threads a column
+__global__ void __launch_bounds__(256) layer_norm_sum_kernel(const float* __restrict__ partial, int n, int C, float* dw, float* db) {
+  __shared__ float red[8][33];
+  griddep_wait();
+  griddep_launch_dependents();
+  const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
+  const int c = blockIdx.x * 32 + lane;
+  float s = 0.f;
+  if (c < 2 * C) {
+#pragma unroll 8
+    for (int i = part; i < n; i += 8) s += __ldcg(partial + (size_t)i * 2 * C + c);
+  }
+  red[part][lane] = s;
+  __syncthreads();
+  if (part == 0 && c < 2 * C) {
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += red[i][lane];
+    if (c < C) {
+      if (dw) dw[c] = s;
+    } else if (db) {
+      db[c - C] = s;
+    }
+  }
+}
+
+constexpr int kWarpCols = 1024;         // longest row that one warp takes
+constexpr int kNormWarps = 4;           // warps of a block that take a row each
+
+int norm_block_warps(int C) { return (C + kWarpCols - 1) / kWarpCols; }
+
+// 16-byte pieces where every row starts on such a boundary, single values elsewhere
+bool norm_wide(const NormArgs& a) {
+  const size_t e = a.dtype == JV_F32 ? 4 : 2;
+  const uintptr_t low = (uintptr_t)a.x | (uintptr_t)a.dy | (uintptr_t)a.y | (uintptr_t)a.w | (uintptr_t)a.b | a.C * e | a.x_stride * e | a.dy_stride * e;
+  return low % 16 == 0;
+}
+
+template <typename T, int VEC, bool GRAD>
+cudaError_t launch_norm(const NormArgs& a, const NormParams& p, int blocks, cudaStream_t st) {
+  constexpr int kAll = 32 / VEC;        // pieces of a lane that holds 32 values
+  auto go = [&](auto kernel, bool block) -> cudaError_t {
+    const int warps = block ? norm_block_warps(a.C) : kNormWarps;
+    const size_t smem = !GRAD ? 0 : block ? 128 * sizeof(float) : 2 * (size_t)a.C * sizeof(float);
+    return launch_programmatic(kernel, dim3((unsigned)blocks), warps * 32, smem, st, p);
+  };
+  if (a.C > kWarpCols) return go(GRAD ? layer_norm_grad_kernel<T, VEC, kAll, true> : layer_norm_kernel<T, VEC, kAll, true>, true);
+  const int quarter = (a.C + 255) / 256;                 // 8, 16, 24 or 32 values a lane
+  switch (quarter) {
+    case 1: return go(GRAD ? layer_norm_grad_kernel<T, VEC, kAll / 4, false> : layer_norm_kernel<T, VEC, kAll / 4, false>, false);
+    case 2: return go(GRAD ? layer_norm_grad_kernel<T, VEC, kAll / 2, false> : layer_norm_kernel<T, VEC, kAll / 2, false>, false);
+    case 3: return go(GRAD ? layer_norm_grad_kernel<T, VEC, kAll / 4 * 3, false> : layer_norm_kernel<T, VEC, kAll / 4 * 3, false>, false);
+    default: return go(GRAD ? layer_norm_grad_kernel<T, VEC, kAll, false> : layer_norm_kernel<T, VEC, kAll, false>, false);
+  }
+}
+
+template <bool GRAD>
+cudaError_t dispatch_norm(const NormArgs& a, const NormParams& p, int blocks, cudaStream_t st) {
+  const bool wide = norm_wide(a);
+  if (a.dtype == JV_F32) return wide ? launch_norm<float, 4, GRAD>(a, p, blocks, st) : launch_norm<float, 1, GRAD>(a, p, blocks, st);
+  return wide ? launch_norm<__nv_bfloat16, 8, GRAD>(a, p, blocks, st) : launch_norm<__nv_bfloat16, 1, GRAD>(a, p, blocks, st);
+}
+
+}  // namespace
+
+int layer_norm_grad_blocks(int64_t rows, int C) {
+  const int64_t per_block = C > kWarpCols ? 1 : kNormWarps;
+  const int64_t most = C > kWarpCols ? 2ll * device_sm_count() : 3ll * device_sm_count(), need = (rows + per_block - 1) / per_block;
+  return (int)(need < most ? need : most);
+}
+
+cudaError_t launch_layer_norm(const NormArgs& a, cudaStream_t st) {
+  const NormParams p{a.x, nullptr, a.w, a.b, a.y, a.mean, a.rstd, nullptr, a.rows, a.x_stride, 0, a.C, a.eps};
+  const int64_t blocks = a.C > kWarpCols ? a.rows : (a.rows + kNormWarps - 1) / kNormWarps;
+  return dispatch_norm<false>(a, p, (int)blocks, st);
+}
+
+cudaError_t launch_layer_norm_grad(const NormArgs& a, float* partial, float* dw, float* db, cudaStream_t st) {
+  const bool sums = dw || db;
+  const int blocks = layer_norm_grad_blocks(a.rows, a.C);
+  const NormParams p{a.x, a.dy, a.w, nullptr, a.y, a.mean, a.rstd, sums ? partial : nullptr, a.rows, a.x_stride, a.dy_stride, a.C, 0.f};
+  const cudaError_t e = dispatch_norm<true>(a, p, blocks, st);
+  if (e != cudaSuccess || !sums) return e;
+  return launch_programmatic(layer_norm_sum_kernel, dim3((unsigned)ceil_div(2 * a.C, 32)), 256, 0, st, (const float*)partial, blocks, a.C, dw, db);
+}
+
+}  // namespace jv

@@ -31,6 +31,11 @@ class JvDwc(ctypes.Structure):
                 ("token_wise", ctypes.c_int32)]
 
 
+class JvNormShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("C", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("x_stride", ctypes.c_int64), ("dy_stride", ctypes.c_int64)]
+
+
 _DwcPtrs = ctypes.POINTER(ctypes.POINTER(JvDwc))
 
 
@@ -70,8 +75,13 @@ def lib() -> ctypes.CDLL:
         L.jv_selftest_wait_timeout.restype = ctypes.c_int
         L.jv_qkv_proj.argtypes = [vp, vp, vp, vp, vp, vp, shp, vp]
         L.jv_out_proj.argtypes = [vp, vp, vp, vp, shp, vp]
+        nshp = ctypes.POINTER(JvNormShape)
+        L.jv_layer_norm.argtypes = [vp, vp, vp, vp, vp, vp, nshp, f32, vp]
+        L.jv_layer_norm_grad_workspace_bytes.argtypes = [nshp]
+        L.jv_layer_norm_grad_workspace_bytes.restype = sz
+        L.jv_layer_norm_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, nshp, vp, sz, vp]
         for f in (L.jv_linear_attn, L.jv_window_attn, L.jv_full_attn, L.jv_hybrid_mixers, L.jv_device_status,
-                  L.jv_qkv_proj, L.jv_out_proj):
+                  L.jv_qkv_proj, L.jv_out_proj, L.jv_layer_norm, L.jv_layer_norm_grad):
             f.restype = ctypes.c_int
         L.jv_set_force_generic.argtypes = [i32]
         L.jv_set_force_generic.restype = i32
@@ -391,6 +401,92 @@ def out_proj(o, w, bias, Hg: int, Wg: int, out=None, stream=None, prefix: int = 
                                ctypes.byref(shape), _stream(stream))
     _raise(st, "jv_out_proj")
     return y
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _f32_on(t: Optional[torch.Tensor], shape, device, what: str):
+    """``t`` (or None) has to be a contiguous fp32 tensor of that shape on the call's device."""
+    if t is not None and not (t.is_cuda and t.device == device and t.dtype == torch.float32 and t.is_contiguous()
+                              and tuple(t.shape) == tuple(shape)):
+        raise ValueError(f"{what} must be a contiguous fp32 CUDA tensor of {list(shape)} on the call's device")
+
+
+def _rows(t: torch.Tensor, what: str):
+    """(rows, C, elements between rows) of a [..., C] tensor whose rows lie evenly spaced."""
+    if not t.is_cuda:
+        raise ValueError("tensors must live on a CUDA device (there is no CPU path)")
+    if t.dim() < 1 or t.numel() == 0:
+        raise ValueError(f"{what} must be a [..., C] tensor that is not empty")
+    C = t.shape[-1]
+    if t.is_contiguous():
+        return t.numel() // C, C, C
+    try:
+        flat = t.view(-1, C)
+    except RuntimeError:
+        flat = None
+    if flat is None or (C > 1 and flat.stride(1) != 1) or (flat.shape[0] > 1 and flat.stride(0) < C):
+        raise ValueError(f"the rows of {what} must be contiguous, evenly spaced and apart from each other")
+    return flat.shape[0], C, flat.stride(0) if flat.shape[0] > 1 else C
+
+
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-6, out=None, stats=None, stream=None) -> torch.Tensor:
+    """jv_layer_norm over the last axis of ``x`` (f32 or bf16, [..., C]; rows evenly spaced); ``weight`` and ``bias`` fp32 [C] or
+    None.  ``stats``: an optional pair of fp32 tensors of one element per row that receive mean and 1 / standard
+    deviation, which layer_norm_grad takes."""
+    rows, C, stride = _rows(x, "x")
+    shape = JvNormShape(rows, C, _dtype_code(x), stride, 0)
+    _f32_on(weight, (C,), x.device, "weight")
+    _f32_on(bias, (C,), x.device, "bias")
+    mean, rstd = stats if stats is not None else (None, None)
+    if stats is not None:
+        for t in (mean, rstd):
+            if t.numel() != rows:
+                raise ValueError("stats must hold one element per row")
+            _f32_on(t, t.shape, x.device, "stats")
+    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    if not (out.is_cuda and out.is_contiguous() and out.shape == x.shape and out.dtype == x.dtype and out.device == x.device):
+        raise ValueError("out must be a contiguous tensor of x's shape, dtype and device")
+    with _current_device(x.device):
+        st = lib().jv_layer_norm(x.data_ptr(), _ptr(weight), _ptr(bias), out.data_ptr(), _ptr(mean), _ptr(rstd),
+                                 ctypes.byref(shape), float(eps), _stream(stream))
+    _raise(st, "jv_layer_norm")
+    return out
+
+
+def layer_norm_grad(dy, x, weight, mean, rstd, weight_grad: bool = True, bias_grad: bool = True, out=None,
+                    ws: Optional[torch.Tensor] = None, stream=None):
+    """jv_layer_norm_grad: (dx, dw, db) of layer_norm from ``dy`` and what the forward pass left in ``stats``.  dw and db are fp32
+    [C], None where not wanted.  ``out``: an optional (dx, dw, db) to write into."""
+    rows, C, stride = _rows(x, "x")
+    if dy.shape != x.shape or dy.dtype != x.dtype or dy.device != x.device:
+        raise ValueError("dy must have x's shape, dtype and device")
+    shape = JvNormShape(rows, C, _dtype_code(x), stride, _rows(dy, "dy")[2])
+    _f32_on(weight, (C,), x.device, "weight")
+    for t in (mean, rstd):
+        if t is None or t.numel() != rows:
+            raise ValueError("mean and rstd must hold one element per row")
+        _f32_on(t, t.shape, x.device, "mean and rstd")
+    if out is None:
+        new = lambda want: torch.empty(C, dtype=torch.float32, device=x.device) if want else None
+        out = (torch.empty(x.shape, dtype=x.dtype, device=x.device), new(weight_grad), new(bias_grad))
+    dx, dw, db = out
+    if not (dx.is_cuda and dx.is_contiguous() and dx.shape == x.shape and dx.dtype == x.dtype and dx.device == x.device):
+        raise ValueError("dx must be a contiguous tensor of x's shape, dtype and device")
+    _f32_on(dw, (C,), x.device, "dw")
+    _f32_on(db, (C,), x.device, "db")
+    with _current_device(x.device):
+        if ws is None and (dw is not None or db is not None):
+            ws = torch.empty(int(lib().jv_layer_norm_grad_workspace_bytes(ctypes.byref(shape))), dtype=torch.uint8, device=x.device)
+            if stream is not None:
+                ws.record_stream(stream)
+        wp, wn = _ws_args(ws)
+        st = lib().jv_layer_norm_grad(dy.data_ptr(), x.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(),
+                                      _ptr(dw), _ptr(db), ctypes.byref(shape), wp, wn, _stream(stream))
+    _raise(st, "jv_layer_norm_grad")
+    return dx, dw, db
 
 
 def selftest_wait_timeout(limit_us: int, gave_up: Optional[torch.Tensor] = None, stream=None) -> None:
