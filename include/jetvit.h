@@ -288,6 +288,86 @@ jv_status jv_layer_norm_grad(const void* dy, const void* x, const float* w, cons
                              float* dw, float* db, const jv_norm_shape* shape, void* ws, size_t ws_bytes, void* cuda_stream);
 
 /*
+ * Differential attention: a softmax mixer whose weights are the difference of two softmax maps, on the arrays that F works on.
+ * Heads come in pairs; pair p has the maps of heads 2p and 2p + 1 of q and k, and the value rows of heads 2p and 2p + 1 of v
+ * side by side (2 D channels); its result takes the place of heads 2p and 2p + 1 of o:
+ *   x_i = sum_j (P0_ij - lambda P1_ij) v_j,   Pm_i = softmax over the keys j that query i sees of  scale q_(2p+m),i . k_(2p+m),j
+ *   lambda = exp(lq1 . lk1) - exp(lq2 . lk2) + lambda_init,        the four learned vectors: rows of lambda [4, D], fp32
+ *   o_i = (1 - lambda_init) norm_w x_i / sqrt(mean x_i^2 + norm_eps)  with norm_w (fp32 [2 D], mean over the pair's 2 D
+ *   channels); o_i = x_i where norm_w is NULL.
+ * q is [B, H, Nq, D], k and v [B, Hkv, Nk, D] (H a multiple of Hkv, both even: H / Hkv pairs of queries share a pair of keys), o
+ * [B, H, Nq, D] contiguous.  q_stride and kv_stride (k and v alike) give the elements between {tokens, heads, batch elements};
+ * all zero: contiguous.  The channels of a row are contiguous; strides are positive multiples of 16 bytes.
+ *   kv_len  device int32 [B] or NULL: keys j >= kv_len[b] do not exist (Nk bounds it, below 0 counts as 0).  Their memory may
+ *           hold anything.
+ *   causal  query i sees the keys j <= q_pos[b] + i only; q_pos device int32 [B] or NULL: Nk - Nq, the queries being the last of
+ *           the Nk positions (0 for a whole prompt).  A key that a query does not see weighs exactly nothing or less than 2^-125
+ *           of what it does see, so finite values of v do not reach it; infinities and NaN among the rows of v below kv_len may.
+ * All rows of o are written.  A query that sees no key gets zeros.  As everywhere in this library a key of score -inf weighs
+ * nothing, a row that sees keys but none of weight is NaN, and a score of +inf or NaN makes its row NaN.
+ * bf16 tensors with D = 64: tensor cores, fp32 softmax and sums, one rounding of P to bf16 and one of o.  f32, and bf16 with other
+ * D <= 64: fp32 arithmetic (row * element size a multiple of 16 bytes).  scale <= 0 selects 1/sqrt(D).
+ * Few queries (single tokens against a cache) and prompts take different kernels; both spread the keys over the whole GPU whatever
+ * the lengths are.  ws must cover jv_diff_attn_workspace_bytes() (0 on invalid arguments), 256-byte aligned.
+ */
+typedef struct {
+  int32_t B, H, Hkv, Nq, Nk, D;
+  int32_t dtype;          /* jv_dtype of q, k, v, o */
+  int32_t causal;         /* 0 or 1 */
+  int64_t q_stride[3];
+  int64_t kv_stride[3];
+} jv_diff_shape;
+typedef struct {
+  const float* lambda;    /* [4, D]: lq1, lk1, lq2, lk2 */
+  float lambda_init;
+  const float* norm_w;    /* [2 D] or NULL */
+  float norm_eps;
+  const int32_t* kv_len;  /* [B] or NULL */
+  const int32_t* q_pos;   /* [B] or NULL */
+} jv_diff;
+size_t jv_diff_attn_workspace_bytes(const jv_diff_shape* shape);
+jv_status jv_diff_attn(const void* q, const void* k, const void* v, void* o, const jv_diff_shape* shape, const jv_diff* diff,
+                       float scale, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/*
+ * The short causal convolution of a state-space mixer, one filter per channel over a token and the K - 1 before it:
+ *   u[b, t, c] = act(bias[c] + sum_(j < K) w[c, j] x[b, t - (K - 1) + j, c]),  act(x) = x / (1 + exp(-x)) with silu = 1, x with 0
+ * x is [B, L, C] with x_stride elements between {token rows, batch elements} (0: C; L rows), u [B, L, C] contiguous,
+ * both of shape.dtype; w fp32 [C, K], 2 <= K <= 4, bias fp32 [C] or NULL.  What precedes the first token is state_in [B, K - 1, C]
+ * (shape.dtype, oldest first), zeros if NULL.  state_out, if not NULL, receives the last K - 1 inputs; it may be state_in itself.
+ * lens: device int32 [B] or NULL.  Sequence b has lens[b] tokens (0 .. L); rows of u behind them are left as they are, and the state is
+ * that behind its last token.  L = 1 is the single-token form.
+ */
+typedef struct {
+  int32_t B, L, C, K;
+  int32_t dtype, silu;
+  int64_t x_stride[2];
+} jv_conv_shape;
+jv_status jv_causal_conv(const void* x, const float* w, const float* bias, const void* state_in, void* u, void* state_out,
+                         const int32_t* lens, const jv_conv_shape* shape, void* cuda_stream);
+
+/*
+ * The selective scan of a state-space mixer, a linear-time mixer beside L: every channel carries Ns states through the sequence,
+ *   d_t = softplus(dt_t + dt_bias)  (softplus = 0: the sum itself),
+ *   h_t[n] = exp(d_t A[n]) h_(t-1)[n] + d_t B_t[n] u_t,      y_t = (sum_n C_t[n] h_t[n] + D u_t) * z_t / (1 + exp(-z_t))
+ * u, dt, z are [B, L, C], Bm and Cm [B, L, Ns] (shared by the channels), y [B, L, C] contiguous, all of shape.dtype; A fp32 [C, Ns],
+ * D and dt_bias fp32 [C] or NULL, z NULL: no gate.  The strides are elements between {token rows, batch elements} (0: contiguous
+ * rows; L rows).  state_in fp32 [B, C, Ns] or NULL (zeros), state_out receives the state behind the last token if not
+ * NULL; it may be state_in itself.  lens as for jv_causal_conv.  1 <= Ns <= 64.  States and sums in fp32.
+ * Long sequences of few channels are cut into chunks whose states pass through ws (jv_selective_scan_workspace_bytes(), 0 where none is
+ * needed or the arguments are invalid; 256-byte aligned).  L = 1 is the single-token form.
+ */
+typedef struct {
+  int32_t B, L, C, Ns;
+  int32_t dtype, softplus;
+  int64_t u_stride[2], dt_stride[2], b_stride[2], c_stride[2], z_stride[2];
+} jv_scan_shape;
+size_t jv_selective_scan_workspace_bytes(const jv_scan_shape* shape);
+jv_status jv_selective_scan(const void* u, const void* dt, const float* A, const void* Bm, const void* Cm, const float* D,
+                            const void* z, const float* dt_bias, const float* state_in, void* y, float* state_out,
+                            const int32_t* lens, const jv_scan_shape* shape, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/*
  * Synchronises the stream, then returns and clears the sticky device status:
  * JV_OK, JV_ERR_TIMEOUT if a kernel abandoned a bounded wait since the last
  * call, or JV_ERR_CUDA if the stream reports a CUDA error.

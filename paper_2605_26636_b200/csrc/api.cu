@@ -1,12 +1,15 @@
 // C ABI of libjetvit: argument validation, dispatch, device status.
 // Every argument error is reported before anything is launched.
 #include <atomic>
+#include <initializer_list>
 #include <math.h>
 #include <stdio.h>
 #include <stdlib.h>
 #include <string.h>
 
+#include "attn_diff.cuh"
 #include "common.cuh"
+#include "scan.cuh"
 
 namespace jv {
 namespace {
@@ -148,6 +151,68 @@ jv_status check_norm(const jv_norm_shape* s) {
 size_t norm_rows_bytes(const jv_norm_shape* s, int64_t stride) {
   return (size_t)((s->rows - 1) * (stride ? stride : s->C) + s->C) * (s->dtype == JV_F32 ? 4 : 2);
 }
+
+// {token rows, batch elements} of a [B, L, C] tensor; false if token rows would overlap or run backwards
+bool token_rows(const int64_t* s, int L, int C, Rows* out) {
+  out->tok = s[0] ? s[0] : C;
+  out->batch = s[1] ? s[1] : L * out->tok;
+  return out->tok >= C && out->batch > 0;
+}
+bool far_rows(const Rows& r) { return r.tok > (int64_t)1 << 31 || r.batch > (int64_t)1 << 55; }
+
+// {tokens, heads, batch elements}; a zero entry only where all are zero (contiguous)
+bool diff_strides(const int64_t* s, int heads, int n, int D, InStrides* out) {
+  if (!s[0] && !s[1] && !s[2]) {
+    *out = InStrides{(int64_t)D, (int64_t)n * D, (int64_t)heads * n * D};
+    return true;
+  }
+  *out = InStrides{s[0], s[1], s[2]};
+  return s[0] > 0 && s[1] > 0 && s[2] > 0;
+}
+size_t diff_bytes(const InStrides& s, int B, int heads, int n, int D, size_t e) {
+  return (size_t)((B - 1) * s.batch + (heads - 1) * s.head + (n - 1) * s.tok + D) * e;
+}
+jv_status check_diff(const jv_diff_shape* s, InStrides* qs, InStrides* ks) {
+  if (!s || s->B <= 0 || s->H <= 0 || s->Hkv <= 0 || s->Nq <= 0 || s->Nk <= 0 || s->D <= 0) return JV_ERR_INVALID_ARG;
+  if (s->dtype != JV_F32 && s->dtype != JV_BF16) return JV_ERR_INVALID_ARG;
+  if (s->causal != 0 && s->causal != 1) return JV_ERR_INVALID_ARG;
+  if (s->H % 2 || s->Hkv % 2 || s->H % s->Hkv) return JV_ERR_INVALID_ARG;
+  if (s->Nq > (1 << 24) || s->Nk > (1 << 24) || (int64_t)s->B * s->H > 65535 || s->D > 64) return JV_ERR_UNSUPPORTED;
+  const int64_t e = s->dtype == JV_F32 ? 4 : 2;
+  if (s->D * e % 16) return JV_ERR_UNSUPPORTED;
+  if (!diff_strides(s->q_stride, s->H, s->Nq, s->D, qs) || !diff_strides(s->kv_stride, s->Hkv, s->Nk, s->D, ks)) return JV_ERR_INVALID_ARG;
+  for (const InStrides* x : {qs, ks})
+    for (int64_t v : {x->tok, x->head, x->batch}) {
+      if (v * e % 16) return JV_ERR_INVALID_ARG;
+      if (v > (int64_t)1 << 37) return JV_ERR_UNSUPPORTED;
+    }
+  return JV_OK;
+}
+
+jv_status check_conv(const jv_conv_shape* s, Rows* xs) {
+  if (!s || s->B <= 0 || s->L <= 0 || s->C <= 0 || s->K <= 0) return JV_ERR_INVALID_ARG;
+  if (s->dtype != JV_F32 && s->dtype != JV_BF16) return JV_ERR_INVALID_ARG;
+  if ((s->silu != 0 && s->silu != 1) || !token_rows(s->x_stride, s->L, s->C, xs)) return JV_ERR_INVALID_ARG;
+  if (s->K < 2 || s->K > 4 || s->B > 65535 || s->C > (1 << 20) || s->L > (1 << 24) || far_rows(*xs)) return JV_ERR_UNSUPPORTED;
+  return (int64_t)s->B * s->L * s->C > ((int64_t)1 << 40) ? JV_ERR_UNSUPPORTED : JV_OK;
+}
+
+struct ScanRows {
+  Rows u, dt, b, c, z;
+};
+jv_status check_scan(const jv_scan_shape* s, ScanRows* r) {
+  if (!s || s->B <= 0 || s->L <= 0 || s->C <= 0 || s->Ns <= 0) return JV_ERR_INVALID_ARG;
+  if (s->dtype != JV_F32 && s->dtype != JV_BF16) return JV_ERR_INVALID_ARG;
+  if (s->softplus != 0 && s->softplus != 1) return JV_ERR_INVALID_ARG;
+  if (!token_rows(s->u_stride, s->L, s->C, &r->u) || !token_rows(s->dt_stride, s->L, s->C, &r->dt) || !token_rows(s->z_stride, s->L, s->C, &r->z) ||
+      !token_rows(s->b_stride, s->L, s->Ns, &r->b) || !token_rows(s->c_stride, s->L, s->Ns, &r->c))
+    return JV_ERR_INVALID_ARG;
+  for (const Rows& v : {r->u, r->dt, r->b, r->c, r->z})
+    if (far_rows(v)) return JV_ERR_UNSUPPORTED;
+  if (s->Ns > 64 || s->B > 65535 || s->C > (1 << 20) || s->L > (1 << 24)) return JV_ERR_UNSUPPORTED;
+  return JV_OK;
+}
+size_t token_rows_bytes(int B, int L, const Rows& r, int C, size_t e) { return (size_t)(r.at(B - 1, L - 1) + C) * e; }
 
 float pick_scale(float scale, int D) { return scale > 0.f ? scale : 1.f / sqrtf((float)D); }
 
@@ -453,6 +518,87 @@ jv_status jv_layer_norm_grad(const void* dy, const void* x, const float* w, cons
   const NormArgs a{x, dy, w, nullptr, dx, const_cast<float*>(mean), const_cast<float*>(rstd), shape->rows,
                    shape->x_stride ? shape->x_stride : shape->C, shape->dy_stride ? shape->dy_stride : shape->C, shape->C, shape->dtype, 0.f};
   return from_cuda(launch_layer_norm_grad(a, (float*)ws, dw, db, (cudaStream_t)cuda_stream));
+}
+
+size_t jv_diff_attn_workspace_bytes(const jv_diff_shape* shape) {
+  InStrides qs, ks;
+  if (check_diff(shape, &qs, &ks) != JV_OK) return 0;
+  return diff_workspace_bytes(shape->B, shape->H / 2, shape->Hkv / 2, shape->Nq, shape->Nk, shape->D, shape->dtype, shape->causal != 0);
+}
+
+jv_status jv_diff_attn(const void* q, const void* k, const void* v, void* o, const jv_diff_shape* shape, const jv_diff* diff,
+                       float scale, void* ws, size_t ws_bytes, void* cuda_stream) {
+  InStrides qs, ks;
+  jv_status st = check_diff(shape, &qs, &ks);
+  if (st != JV_OK) return st;
+  if (!q || !k || !v || !o || !diff || !diff->lambda) return JV_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(o, 16)) return JV_ERR_INVALID_ARG;
+  if (!aligned(diff->lambda, 4) || !aligned(diff->norm_w, 16) || !aligned(diff->kv_len, 4) || !aligned(diff->q_pos, 4)) return JV_ERR_INVALID_ARG;
+  if (!isfinite(diff->lambda_init) || (diff->norm_w && !(diff->norm_eps >= 0.f))) return JV_ERR_INVALID_ARG;
+  const int B = shape->B, D = shape->D;
+  const size_t e = shape->dtype == JV_F32 ? 4 : 2, need = jv_diff_attn_workspace_bytes(shape), nkv = diff_bytes(ks, B, shape->Hkv, shape->Nk, D, e);
+  const Span in[7] = {{q, diff_bytes(qs, B, shape->H, shape->Nq, D, e)}, {k, nkv}, {v, nkv}, {diff->lambda, (size_t)16 * D},
+                      {diff->norm_w, (size_t)8 * D}, {diff->kv_len, (size_t)4 * B}, {diff->q_pos, (size_t)4 * B}};
+  const Span out[2] = {{o, (size_t)B * shape->H * shape->Nq * D * e}, {need ? ws : nullptr, need}};
+  if (outputs_clash(in, 7, out, 2)) return JV_ERR_INVALID_ARG;
+  if ((st = check_ws(ws, ws_bytes, need)) != JV_OK) return st;
+  if ((st = check_device()) != JV_OK) return st;
+  const DiffArgs a{q, k, v, o, B, shape->H / 2, shape->Hkv / 2, shape->Nq, shape->Nk, D, shape->dtype, shape->causal != 0, qs, ks,
+                   diff->lambda, diff->lambda_init, diff->norm_w, diff->norm_eps, diff->kv_len, diff->q_pos, pick_scale(scale, D)};
+  return from_cuda(launch_diff_generic(a, (cudaStream_t)cuda_stream));
+}
+
+jv_status jv_causal_conv(const void* x, const float* w, const float* bias, const void* state_in, void* u, void* state_out,
+                         const int32_t* lens, const jv_conv_shape* shape, void* cuda_stream) {
+  Rows xs;
+  jv_status st = check_conv(shape, &xs);
+  if (st != JV_OK) return st;
+  const size_t e = shape->dtype == JV_F32 ? 4 : 2;
+  if (!x || !w || !u) return JV_ERR_INVALID_ARG;
+  if (!aligned(x, e) || !aligned(u, e) || !aligned(state_in, e) || !aligned(state_out, e) || !aligned(w, 4) || !aligned(bias, 4) || !aligned(lens, 4))
+    return JV_ERR_INVALID_ARG;
+  const int B = shape->B, L = shape->L, C = shape->C, K = shape->K;
+  const size_t state = (size_t)B * (K - 1) * C * e;
+  const Span in[5] = {{x, token_rows_bytes(B, L, xs, C, e)}, {w, (size_t)C * K * 4}, {bias, (size_t)C * 4}, {lens, (size_t)B * 4},
+                      {state_in == state_out ? nullptr : state_in, state}};
+  const Span out[2] = {{u, (size_t)B * L * C * e}, {state_out, state}};
+  if (outputs_clash(in, 5, out, 2) || (state_in && overlaps(u, out[0].bytes, state_in, state))) return JV_ERR_INVALID_ARG;
+  if ((st = check_device()) != JV_OK) return st;
+  const ConvArgs a{x, w, bias, state_in, u, state_out, lens, B, L, C, K, shape->dtype, shape->silu, xs};
+  return from_cuda(launch_causal_conv(a, (cudaStream_t)cuda_stream));
+}
+
+size_t jv_selective_scan_workspace_bytes(const jv_scan_shape* shape) {
+  ScanRows r;
+  if (check_scan(shape, &r) != JV_OK) return 0;
+  return scan_plan(shape->B, shape->L, shape->C, shape->Ns).total;
+}
+
+jv_status jv_selective_scan(const void* u, const void* dt, const float* A, const void* Bm, const void* Cm, const float* D,
+                            const void* z, const float* dt_bias, const float* state_in, void* y, float* state_out,
+                            const int32_t* lens, const jv_scan_shape* shape, void* ws, size_t ws_bytes, void* cuda_stream) {
+  ScanRows r;
+  jv_status st = check_scan(shape, &r);
+  if (st != JV_OK) return st;
+  const size_t e = shape->dtype == JV_F32 ? 4 : 2;
+  if (!u || !dt || !A || !Bm || !Cm || !y) return JV_ERR_INVALID_ARG;
+  for (const void* p : {u, dt, Bm, Cm, z, (const void*)y})
+    if (!aligned(p, e)) return JV_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)A, (const void*)D, (const void*)dt_bias, (const void*)state_in, (const void*)state_out, (const void*)lens})
+    if (!aligned(p, 4)) return JV_ERR_INVALID_ARG;
+  const int B = shape->B, L = shape->L, C = shape->C, Ns = shape->Ns;
+  const size_t state = (size_t)B * C * Ns * 4;
+  const ScanPlan plan = scan_plan(B, L, C, Ns);
+  const Span in[10] = {{u, token_rows_bytes(B, L, r.u, C, e)}, {dt, token_rows_bytes(B, L, r.dt, C, e)}, {Bm, token_rows_bytes(B, L, r.b, Ns, e)},
+                       {Cm, token_rows_bytes(B, L, r.c, Ns, e)}, {z, token_rows_bytes(B, L, r.z, C, e)}, {A, (size_t)C * Ns * 4},
+                       {D, (size_t)C * 4}, {dt_bias, (size_t)C * 4}, {lens, (size_t)B * 4}, {state_in == state_out ? nullptr : state_in, state}};
+  const Span out[3] = {{y, (size_t)B * L * C * e}, {state_out, state}, {plan.total ? ws : nullptr, plan.total}};
+  if (outputs_clash(in, 10, out, 3)) return JV_ERR_INVALID_ARG;
+  if (state_in && (overlaps(y, out[0].bytes, state_in, state) || (out[2].p && overlaps(ws, plan.total, state_in, state)))) return JV_ERR_INVALID_ARG;
+  if ((st = check_ws(ws, ws_bytes, plan.total)) != JV_OK) return st;
+  if ((st = check_device()) != JV_OK) return st;
+  const ScanArgs a{u, dt, Bm, Cm, z, A, D, dt_bias, state_in, state_out, y, lens, B, L, C, Ns, shape->dtype, shape->softplus, r.u, r.dt, r.b, r.c, r.z};
+  return from_cuda(launch_selective_scan(a, plan, ws, (cudaStream_t)cuda_stream));
 }
 
 jv_status jv_device_status(void* cuda_stream) {

@@ -36,6 +36,25 @@ class JvNormShape(ctypes.Structure):
                 ("x_stride", ctypes.c_int64), ("dy_stride", ctypes.c_int64)]
 
 
+class JvDiffShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "H", "Hkv", "Nq", "Nk", "D", "dtype", "causal")] + [
+        ("q_stride", ctypes.c_int64 * 3), ("kv_stride", ctypes.c_int64 * 3)]
+
+
+class JvDiff(ctypes.Structure):
+    _fields_ = [("lam", ctypes.c_void_p), ("lambda_init", ctypes.c_float), ("norm_w", ctypes.c_void_p),
+                ("norm_eps", ctypes.c_float), ("kv_len", ctypes.c_void_p), ("q_pos", ctypes.c_void_p)]
+
+
+class JvConvShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "L", "C", "K", "dtype", "silu")] + [("x_stride", ctypes.c_int64 * 2)]
+
+
+class JvScanShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "L", "C", "Ns", "dtype", "softplus")] + [
+        (n, ctypes.c_int64 * 2) for n in ("u_stride", "dt_stride", "b_stride", "c_stride", "z_stride")]
+
+
 _DwcPtrs = ctypes.POINTER(ctypes.POINTER(JvDwc))
 
 
@@ -80,8 +99,17 @@ def lib() -> ctypes.CDLL:
         L.jv_layer_norm_grad_workspace_bytes.argtypes = [nshp]
         L.jv_layer_norm_grad_workspace_bytes.restype = sz
         L.jv_layer_norm_grad.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, nshp, vp, sz, vp]
+        dshp, cshp, sshp = ctypes.POINTER(JvDiffShape), ctypes.POINTER(JvConvShape), ctypes.POINTER(JvScanShape)
+        L.jv_diff_attn_workspace_bytes.argtypes = [dshp]
+        L.jv_diff_attn_workspace_bytes.restype = sz
+        L.jv_diff_attn.argtypes = [vp, vp, vp, vp, dshp, ctypes.POINTER(JvDiff), f32, vp, sz, vp]
+        L.jv_causal_conv.argtypes = [vp, vp, vp, vp, vp, vp, vp, cshp, vp]
+        L.jv_selective_scan_workspace_bytes.argtypes = [sshp]
+        L.jv_selective_scan_workspace_bytes.restype = sz
+        L.jv_selective_scan.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sshp, vp, sz, vp]
         for f in (L.jv_linear_attn, L.jv_window_attn, L.jv_full_attn, L.jv_hybrid_mixers, L.jv_device_status,
-                  L.jv_qkv_proj, L.jv_out_proj, L.jv_layer_norm, L.jv_layer_norm_grad):
+                  L.jv_qkv_proj, L.jv_out_proj, L.jv_layer_norm, L.jv_layer_norm_grad, L.jv_diff_attn,
+                  L.jv_causal_conv, L.jv_selective_scan):
             f.restype = ctypes.c_int
         L.jv_set_force_generic.argtypes = [i32]
         L.jv_set_force_generic.restype = i32
@@ -487,6 +515,146 @@ def layer_norm_grad(dy, x, weight, mean, rstd, weight_grad: bool = True, bias_gr
                                       _ptr(dw), _ptr(db), ctypes.byref(shape), wp, wn, _stream(stream))
     _raise(st, "jv_layer_norm_grad")
     return dx, dw, db
+
+
+def _i32_on(t: Optional[torch.Tensor], n: int, device, what: str):
+    if t is not None and not (t.is_cuda and t.device == device and t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n):
+        raise ValueError(f"{what} must be a contiguous int32 CUDA tensor of {n} elements on the call's device")
+
+
+def _head_strides(t: torch.Tensor, what: str):
+    """Elements between {tokens, heads, batch elements} of a [B, H, N, D] tensor; zeros where it is contiguous."""
+    if t.is_contiguous():
+        return 0, 0, 0
+    B, H, N, D = t.shape
+    sb, sh, sn, sd = t.stride()
+    if sd != 1 and D > 1:
+        raise ValueError(f"the channels of {what} must be contiguous")
+    e = max(1, 16 // t.element_size())                 # where there is one of something, any step does
+    sn, sh, sb = (s if n > 1 else max(D, e) for n, s in ((N, sn), (H, sh), (B, sb)))
+    if min(sn, sh, sb) <= 0:
+        raise ValueError(f"{what} must not repeat its rows")
+    return sn, sh, sb
+
+
+def diff_attn(q, k, v, lam, lambda_init: float, norm_weight=None, norm_eps: float = 1e-5, causal: bool = False, kv_len=None,
+              q_pos=None, scale: float = 0.0, out=None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """jv_diff_attn: q [B, H, Nq, D], k and v [B, Hkv, Nk, D], heads in pairs; any strides with contiguous channels, k and v
+    alike.  ``lam``: the four learned vectors, fp32 [4, D]; ``norm_weight``: fp32 [2 D] or None; ``kv_len``, ``q_pos``: int32 [B] or None."""
+    if q.dim() != 4 or k.dim() != 4 or k.shape != v.shape or q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3]:
+        raise ValueError("q must be [B, H, Nq, D], k and v [B, Hkv, Nk, D]")
+    for t in (q, k, v):
+        if not t.is_cuda:
+            raise ValueError("tensors must live on a CUDA device (there is no CPU path)")
+        if t.dtype != q.dtype or t.device != q.device:
+            raise ValueError("q, k and v must have one dtype and device")
+    B, H, Nq, D = q.shape
+    Hkv, Nk = k.shape[1], k.shape[2]
+    ks = _head_strides(k, "k")
+    if _head_strides(v, "v") != ks:
+        raise ValueError("k and v must have the same strides")
+    _f32_on(lam, (4, D), q.device, "lam")
+    _f32_on(norm_weight, (2 * D,), q.device, "norm_weight")
+    _i32_on(kv_len, B, q.device, "kv_len")
+    _i32_on(q_pos, B, q.device, "q_pos")
+    shape = JvDiffShape(B, H, Hkv, Nq, Nk, D, _dtype_code(q), 1 if causal else 0, _head_strides(q, "q"), ks)
+    d = JvDiff(lam.data_ptr(), lambda_init, _ptr(norm_weight), norm_eps, _ptr(kv_len), _ptr(q_pos))
+    out = _empty_out(q) if out is None else out
+    if not (out.is_cuda and out.is_contiguous() and out.shape == q.shape and out.dtype == q.dtype and out.device == q.device):
+        raise ValueError("out must be a contiguous tensor of q's shape, dtype and device")
+    with _current_device(q.device):
+        if ws is None:
+            n = int(lib().jv_diff_attn_workspace_bytes(ctypes.byref(shape)))
+            if n:
+                ws = torch.empty(n, dtype=torch.uint8, device=q.device)
+                if stream is not None:
+                    ws.record_stream(stream)
+        wp, wn = _ws_args(ws)
+        st = lib().jv_diff_attn(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), ctypes.byref(shape), ctypes.byref(d),
+                                float(scale), wp, wn, _stream(stream))
+    _raise(st, "jv_diff_attn")
+    return out
+
+
+def _token_rows(t: Optional[torch.Tensor], B: int, L: int, C: int, like: torch.Tensor, what: str):
+    """Elements between {token rows, batch elements} of a [B, L, C] tensor (zeros: contiguous, or no tensor)."""
+    if t is None:
+        return 0, 0
+    if not t.is_cuda:
+        raise ValueError("tensors must live on a CUDA device (there is no CPU path)")
+    if tuple(t.shape) != (B, L, C) or t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{what} must be [{B}, {L}, {C}], of one dtype and device with the others")
+    if t.is_contiguous():
+        return 0, 0
+    sb, sl, sc = t.stride()
+    row = sl if L > 1 else C
+    batch = sb if B > 1 else L * row
+    if (sc != 1 and C > 1) or row < C or batch <= 0:
+        raise ValueError(f"the token rows of {what} must be contiguous, evenly spaced and apart from each other")
+    return row, batch
+
+
+def _same(t: Optional[torch.Tensor], shape, like: torch.Tensor, what: str):
+    if t is not None and not (t.is_cuda and t.is_contiguous() and tuple(t.shape) == tuple(shape) and t.dtype == like.dtype
+                              and t.device == like.device):
+        raise ValueError(f"{what} must be a contiguous {list(shape)} tensor of the inputs' dtype and device")
+
+
+def causal_conv(x, weight, bias=None, state=None, state_out=None, lens=None, silu: bool = True, out=None, stream=None) -> torch.Tensor:
+    """jv_causal_conv: x [B, L, C] (token rows evenly spaced), ``weight`` fp32 [C, K], ``bias`` fp32 [C] or None; ``state`` (in) and
+    ``state_out`` (may be the same tensor) [B, K - 1, C] of x's dtype; ``lens`` int32 [B].  Rows of ``out`` behind a sequence stay as
+    they are (so pass one where that matters)."""
+    if x.dim() != 3 or weight.dim() != 2:
+        raise ValueError("x must be [B, L, C] and weight [C, K]")
+    B, L, C = x.shape
+    K = weight.shape[1]
+    stride = _token_rows(x, B, L, C, x, "x")
+    _f32_on(weight, (C, K), x.device, "weight")
+    _f32_on(bias, (C,), x.device, "bias")
+    _same(state, (B, K - 1, C), x, "state")
+    _same(state_out, (B, K - 1, C), x, "state_out")
+    _i32_on(lens, B, x.device, "lens")
+    out = torch.empty((B, L, C), dtype=x.dtype, device=x.device) if out is None else out
+    _same(out, (B, L, C), x, "out")
+    shape = JvConvShape(B, L, C, K, _dtype_code(x), 1 if silu else 0, stride)
+    with _current_device(x.device):
+        st = lib().jv_causal_conv(x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(state), out.data_ptr(), _ptr(state_out), _ptr(lens),
+                                  ctypes.byref(shape), _stream(stream))
+    _raise(st, "jv_causal_conv")
+    return out
+
+
+def selective_scan(u, dt, A, Bm, Cm, D=None, z=None, dt_bias=None, state=None, state_out=None, lens=None, softplus: bool = True,
+                   out=None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """jv_selective_scan: u, dt, z [B, L, C], Bm, Cm [B, L, Ns] (token rows evenly spaced), A fp32 [C, Ns], D and dt_bias fp32 [C] or None;
+    ``state`` (in) and ``state_out`` (may be the same tensor) fp32 [B, C, Ns]; ``lens`` int32 [B].  Rows of ``out`` behind a sequence
+    stay as they are."""
+    if u.dim() != 3 or A.dim() != 2:
+        raise ValueError("u must be [B, L, C] and A [C, Ns]")
+    B, L, C = u.shape
+    Ns = A.shape[1]
+    strides = [_token_rows(t, B, L, n, u, what) for t, n, what in ((u, C, "u"), (dt, C, "dt"), (Bm, Ns, "Bm"), (Cm, Ns, "Cm"), (z, C, "z"))]
+    _f32_on(A, (C, Ns), u.device, "A")
+    _f32_on(D, (C,), u.device, "D")
+    _f32_on(dt_bias, (C,), u.device, "dt_bias")
+    _f32_on(state, (B, C, Ns), u.device, "state")
+    _f32_on(state_out, (B, C, Ns), u.device, "state_out")
+    _i32_on(lens, B, u.device, "lens")
+    out = torch.empty((B, L, C), dtype=u.dtype, device=u.device) if out is None else out
+    _same(out, (B, L, C), u, "out")
+    shape = JvScanShape(B, L, C, Ns, _dtype_code(u), 1 if softplus else 0, *strides)
+    with _current_device(u.device):
+        if ws is None:
+            n = int(lib().jv_selective_scan_workspace_bytes(ctypes.byref(shape)))
+            if n:
+                ws = torch.empty(n, dtype=torch.uint8, device=u.device)
+                if stream is not None:
+                    ws.record_stream(stream)
+        wp, wn = _ws_args(ws)
+        st = lib().jv_selective_scan(u.data_ptr(), dt.data_ptr(), A.data_ptr(), Bm.data_ptr(), Cm.data_ptr(), _ptr(D), _ptr(z), _ptr(dt_bias),
+                                     _ptr(state), out.data_ptr(), _ptr(state_out), _ptr(lens), ctypes.byref(shape), wp, wn, _stream(stream))
+    _raise(st, "jv_selective_scan")
+    return out
 
 
 def selftest_wait_timeout(limit_us: int, gave_up: Optional[torch.Tensor] = None, stream=None) -> None:
