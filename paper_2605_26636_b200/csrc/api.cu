@@ -545,6 +545,11 @@ jv_status jv_diff_attn(const void* q, const void* k, const void* v, void* o, con
   if ((st = check_device()) != JV_OK) return st;
   const DiffArgs a{q, k, v, o, B, shape->H / 2, shape->Hkv / 2, shape->Nq, shape->Nk, D, shape->dtype, shape->causal != 0, qs, ks,
                    diff->lambda, diff->lambda_init, diff->norm_w, diff->norm_eps, diff->kv_len, diff->q_pos, pick_scale(scale, D)};
+  if (!g_force_generic.load() && diff_tc_supported(a)) {
+    int* status = device_status_ptr();
+    if (!status) return JV_ERR_CUDA;
+    return from_cuda(launch_diff_tc(a, ws, status, (cudaStream_t)cuda_stream));
+  }
   return from_cuda(launch_diff_generic(a, (cudaStream_t)cuda_stream));
 }
 

@@ -162,5 +162,8 @@ __device__ __forceinline__ float lambda_of(const Tail& t) {
 size_t diff_workspace_bytes(int B, int pairs, int kv_pairs, int Nq, int Nk, int D, int dtype, bool causal);
 // any f32 or bf16 tensors, D <= 64: one warp per query row, fp32 arithmetic
 cudaError_t launch_diff_generic(const DiffArgs& a, cudaStream_t st);
+// bf16, D == 64: tiles of 128 queries on the tensor cores
+bool diff_tc_supported(const DiffArgs& a);
+cudaError_t launch_diff_tc(const DiffArgs& a, void* ws, int* status, cudaStream_t st);
 
 }  // namespace jv

@@ -111,8 +111,6 @@ __global__ void __launch_bounds__(kRowWarps * 32) diff_generic_kernel(const Diff
 
 }  // namespace
 
-size_t diff_workspace_bytes(int, int, int, int, int, int, int, bool) { return 0; }
-
 cudaError_t launch_diff_generic(const DiffArgs& a, cudaStream_t st) {
   const dim3 grid((unsigned)ceil_div(a.Nq, kRowWarps), (unsigned)(a.B * a.pairs));
   if (a.dtype == JV_F32) return launch_programmatic(diff_generic_kernel<float>, grid, kRowWarps * 32, 0, st, a);
