@@ -1,16 +1,24 @@
 // Differential attention on the 5th-generation tensor cores: bf16, 64 channels a map, tiles of 128 queries of a pair of heads.
 //
-// The kernel of head_dim 128 (attn_d128.cu) with its two query tiles turned into the two maps of one: a tile of 128 tokens lies in
-// shared memory as two 128-byte-swizzled halves of 64 channels, the two heads of the pair.  Map m is S_m = Q_m K_m^T over half m alone (4
-// MMAs of K = 16), and both maps multiply the same values, O_m += P_m V over both halves of V (2 x 4 MMAs).  Tensor memory: per
-// map two 64-column score buffers (the bf16 probabilities written over the scores they came from) and one 128-column accumulator,
-// 512 columns.  Warp roles (11 warps): a TMA producer (two buffers of Q, K through a ring of three tiles, V through one of two), an MMA
-// issuer per map, four softmax warps per map, one thread per query row.  Steps of 64 keys, exact two-pass softmax per step
-// against a lazily raised reference.
+// A tile of 128 tokens lies in shared memory as two 128-byte-swizzled halves of 64 channels, the two heads of the pair.  Map m is
+// S_m = Q_m K_m^T over half m alone (4 MMAs of K = 16), and both maps multiply the same values, O_m += P_m V over both halves of V
+// (4 MMAs).  Warp roles (20 warps): a TMA producer, an MMA issuer per map, and four sets of four softmax warps, one thread per query
+// row: set (m, h) takes the steps of 64 keys u = h, h + 2, ... of map m.  Tensor memory, 512 columns: 64 of scores per map, 32
+// of probabilities (bf16) per set, 128 of accumulator per map.
 //
-// Behind an item's last key a thread of map m takes channels 64 m .. 64 m + 63 of its row from both accumulators: the sums of
-// the maps and the shares of the row's mean square are exchanged through shared memory, and the difference is normalised and written as one
-// contiguous row of 128 bytes.  Parts of an item (see attn_diff.cuh) go to the workspace as they are.
+// A set takes its 64 scores a row into registers at once, so the buffer is free for the next step's as soon as they are read: the other
+// set of the map finds them there when it is done with its step before, and neither ever waits for the tensor pipe in the steady
+// state.  (With probabilities over the scores they came from, as the other kernels here have them, the chain  scores -> softmax -> product ->
+// next scores  was in the open a third of the time, with two softmax warps per sub-core or with four: four grids of 73 x 73 tokens, 8
+// pairs, 882 and 856 us.)
+//
+// The two sets of a map add to one accumulator, so they share its reference: a row's reference lies in shared memory, every step looks at
+// it and raises it lazily.  The issuer sees to the order: it issues the scores of step u + 1 when the reference of step u stands, which
+// is also when that step's scores have been read.  Each set keeps its own sum.
+//
+// Behind an item's last key each of a row's four threads takes 32 channels from both accumulators: the sums and the shares of
+// the row's mean square are exchanged through shared memory, the difference is normalised and written.  Parts of an item (see
+// attn_diff.cuh) go to the workspace as they are.
 //
 // Keys that a row does not see are set to -inf behind the load of the scores; rows of V that lie behind a length may hold anything, and
 // are overwritten with zeros in shared memory before the first product of their tile.
@@ -28,15 +36,19 @@ using namespace diff;
 constexpr uint32_t kSuspendNs = 4000;       // suspend-time hint of the barrier waits (tc_common.cuh)
 constexpr int kHalfBytes = kTile * kD * 2;  // one head's half of a tile: 16 KB
 constexpr int kTileBytes = 2 * kHalfBytes;
-constexpr int kQB = 2, kKS = 3, kVS = 2;    // query buffers, ring depths
-constexpr int kWarps = 11;
+constexpr int kQB = 2, kKS = 2, kVS = 2;    // query buffers, ring depths
+constexpr int kWarps = 20;
 constexpr int kThreads = kWarps * 32;
-constexpr int kFirstSoftmaxWarp = 3;
+constexpr int kFirstSoftmaxWarp = 4;
+// Registers: a block is launched with 96 a thread; the first four warps hand back 64 each, the sixteen softmax warps take 16 each, so
+// that a step's 64 scores stay in registers between the maximum and the exponentials
+constexpr int kRegsRoles = 32, kRegsSoftmax = 112;
+static_assert(128 * kRegsRoles + 512 * kRegsSoftmax <= kThreads * 96, "registers of a block");
 constexpr uint32_t kTmemCols = 512;
 constexpr int kSub = 64;                    // keys per step
-constexpr int kPolyOf8 = 3, kPolyDeg = 4;   // of every 8 score pairs, this many take the polynomial exponential, of this degree
-// Tensor-memory columns: score buffer h of map m at 128 m + 64 h, O_m at 256 + 128 m
-constexpr uint32_t kColS = 0, kColO = 256;
+constexpr int kPolyOf8 = 2, kPolyDeg = 3;   // of every 8 score pairs, this many take the polynomial exponential, of this degree
+// Tensor-memory columns: scores of map m at 64 m, probabilities of set s at 128 + 32 s, O_m at 256 + 128 m
+constexpr uint32_t kColS = 0, kColP = 128, kColO = 256;
 
 struct DiffParams {
   Items items;
@@ -52,15 +64,14 @@ struct DiffParams {
 struct __align__(8) Barriers {
   uint64_t q_full[kQB], q_empty[kQB];
   uint64_t k_full[kKS], k_empty[kKS], v_full[kVS], v_empty[kVS];
-  uint64_t s_full[2][2], p_full[2][2];   // per map and score buffer
-  uint64_t pv_done[2];                   // two phases per item: its last but one, its last P V has retired
-  uint64_t sums_in, read_out;            // per item written whole: the maps' sums are there; the accumulators have been read
+  // per map and set, once a step: its scores are there; they have been read and its reference stands; its probabilities are
+  // there; its product has retired
+  uint64_t s_full[2][2], decided[2][2], p_full[2][2], pv_done[2][2];
+  uint64_t sums_in, read_out;            // per item: the sets' sums are there; they and the accumulators have been read
   uint64_t drain;
-  union {
-    long long scan[33];                  // for find_start
-    float swap[2][kTile];                // what the two threads of a row tell each other
-  };
+  long long scan[33];                    // for find_start
   Start start;
+  float ref[2][kTile], base[2][kTile], sum[2][2][kTile], square[4][kTile];   // base: the reference of set (m, 0)'s sum
   uint32_t tmem_base;
   volatile uint32_t abort_flag;
 };
@@ -69,7 +80,12 @@ constexpr size_t kSmemBytes = kSmemTiles + sizeof(Barriers) + 1024;            /
 static_assert(kSmemBytes <= 227 * 1024, "shared memory of one block");
 
 constexpr uint32_t kIdescQK = idesc(kTile, kSub, 0);       // S = Q K^T: M128 N64, both operands K-major
-constexpr uint32_t kIdescPV = idesc(kTile, kD, 1);         // O half = P V half: M128 N64, V MN-major
+constexpr uint32_t kIdescPV = idesc(kTile, kV, 1);         // O = P V: M128 N128, V MN-major
+
+// tcgen05.commit of everything this thread has issued, to be called by one lane
+__device__ __forceinline__ void commit_1(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 
 __global__ void __launch_bounds__(kThreads, 1)
 attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK,
@@ -94,9 +110,10 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
     for (int m = 0; m < 2; ++m) {
       for (int h = 0; h < 2; ++h) {
         mbar_init(&bar->s_full[m][h], 1);
-        mbar_init(&bar->p_full[m][h], 128);
+        mbar_init(&bar->p_full[m][h], 4);       // one arrival from each warp of the set
+        mbar_init(&bar->decided[m][h], 4);
+        mbar_init(&bar->pv_done[m][h], 1);
       }
-      mbar_init(&bar->pv_done[m], 1);
     }
     for (int s = 0; s < kKS; ++s) {
       mbar_init(&bar->k_full[s], 1);
@@ -106,8 +123,8 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
       mbar_init(&bar->v_full[s], 1);
       mbar_init(&bar->v_empty[s], 2);
     }
-    mbar_init(&bar->sums_in, 256);
-    mbar_init(&bar->read_out, 256);
+    mbar_init(&bar->sums_in, 512);
+    mbar_init(&bar->read_out, 512);
     mbar_init(&bar->drain, 2);
     bar->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -141,6 +158,9 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
   }
   Walk it;
   it.begin(bar->start);
+
+  if (warp < kFirstSoftmaxWarp) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsRoles));
+  else asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
 
   if (warp == 0) {
     // ================= TMA producer =================
@@ -184,76 +204,86 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
         while (!mbar_try(&bar->v_full[g % kVS], (g / kVS) & 1) && globaltimer() - t0 < kWaitLimitNs) {}
       while (globaltimer() - t0 < 1000000ull) {}
     }
-  } else if (warp < kFirstSoftmaxWarp) {
+  } else if (warp < 3) {
     // ================= MMA issuer of map x =================
-    // Per item the work is a chain over 64-key steps u (key tile u / 2, half u % 2):
-    //   S(u) = Q_x K_x(u)^T      4 MMAs, M128 N64 K16, operands in shared memory
-    //   O   += P(u) V(u)         2 x 4 MMAs, M128 N64 K16, A = P in tensor memory, one per channel half of V
-    // S(u + 2) goes into the buffer that P(u) V(u) has just read: the tensor pipe executes one thread's MMAs in issue order, so
-    // the commit that publishes S(u + 1) also says that P(u - 1) V(u - 1) has retired; behind the last scores pv_done says so.
+    // Over the block's steps g of 64 keys, one item behind the other (key tile g / 2, half g % 2):
+    //   S(g) = Q_x K_x(g)^T      4 MMAs, M128 N64 K16, operands in shared memory
+    //   O   += P(g) V(g)         4 MMAs, M128 N128 K16, A = P in tensor memory, V from both heads' halves
+    // S(g + 1) is issued when step g has read its scores, the product of step g - 1 behind it; at the first step of an item the other way
+    // round, since its set first has to see the item before to its end.  One election a phase, addresses from running descriptors.
     const int x = warp - 1;
+    const uint32_t dS = tmem + kColS + x * kSub, dP = tmem + kColP + x * kSub, dO = tmem + kColO + x * kV;
+    const uint64_t dQ0 = smem_desc(sQ + x * kHalfBytes), dK0 = smem_desc(sK + x * kHalfBytes);
+    const uint64_t dV0 = (smem_desc(sV) & ~(0x3FFFull << 16)) | ((uint64_t)(kHalfBytes >> 4) << 16);   // the next 64 channels lie kHalfBytes on
     bool ok = true;
-    int n = 0;
-    int sk = 0, sv = 0;                     // ring stages of the score key tile and of the P V key tile
+    Walk itv = it;                          // the products' walk (it: the scores')
+    int qn = 0, sk = 0, sv = 0;             // items of the scores' walk, ring stages of the next key and value tile
     uint32_t phk = 0, phv = 0;              // and their "full" parities
-    uint32_t pcnt[2] = {0, 0};              // publications seen so far per buffer: parity of p_full
-    while (ok && it.next(p.items)) {
-      const int nsteps = 2 * (it.t1 - it.t0), qb = n & 1;
-      const uint64_t dq = smem_desc(sQ + qb * kTileBytes + x * kHalfBytes);
-      auto scores = [&](int u) {
-        const uint64_t dk = smem_desc(sK + sk * kTileBytes + x * kHalfBytes + (u & 1) * (kSub * kD * 2));
-        if (elect_one()) {
-#pragma unroll
-          for (int c = 0; c < kD / 16; ++c)
-            mma_ss_1(tmem + kColS + x * 128 + (u & 1) * kSub, desc_advance(dq, c * 32), desc_advance(dk, c * 32), kIdescQK, c > 0 ? 1u : 0u);
-        }
-        __syncwarp();
-        tc_commit(&bar->s_full[x][u & 1]);
-        if ((u & 1) == 1) {
-          tc_commit(&bar->k_empty[sk]);
-          if (++sk == kKS) { sk = 0; phk ^= 1; }
-        }
-        if (u == nsteps - 1) tc_commit(&bar->q_empty[qb]);    // the item's last scores: its query tile may be replaced
-      };
-      auto key_landed = [&](int u) -> bool {
-        return (u & 1) == 1 || warp_wait<kSuspendNs>(&bar->k_full[sk], phk, &bar->abort_flag, p.status);
-      };
-      ok = warp_wait<kSuspendNs>(&bar->q_full[qb], (n >> 1) & 1, &bar->abort_flag, p.status);
-      ++n;
-      for (int u = 0; u < 2 && ok; ++u) {   // (a key tile is two steps: nsteps >= 2)
-        ok = key_landed(u);
-        if (!ok) break;
-        tc_fence_after();
-        scores(u);
+    int s_left = 0, v_left = 0;             // steps left of the walks' items
+    bool v_first = false;                   // the next product is an item's first
+    // Scores of the next step, of half h of its tile; false if there is none (or the wait has run out: ok)
+    auto next_scores = [&](uint32_t h) -> bool {
+      if (s_left == 0) {
+        if (!it.next(p.items)) return false;
+        s_left = 2 * (it.t1 - it.t0);
+        ok = warp_wait<kSuspendNs>(&bar->q_full[qn & 1], (qn >> 1) & 1, &bar->abort_flag, p.status);
+        if (!ok) return false;
+        ++qn;
       }
-      for (int u = 0; u < nsteps && ok; ++u) {
-        const int hb = u & 1;
-        const bool more = u + 2 < nsteps;   // the buffer of step u is free behind its P V: the scores of step u + 2 go there
-        if (hb == 0) ok = warp_wait<kSuspendNs>(&bar->v_full[sv], phv, &bar->abort_flag, p.status);   // P V of a first half: its V must have landed
-        if (ok && more) ok = key_landed(u + 2);
-        if (ok) ok = warp_wait<kSuspendNs>(&bar->p_full[x][hb], pcnt[hb] & 1, &bar->abort_flag, p.status);
-        if (!ok) break;
-        ++pcnt[hb];
-        const uint32_t vb = sV + sv * kTileBytes + hb * (kSub * kD * 2);
-        tc_fence_after();
-        if (elect_one()) {                 // one lane issues the step's MMAs back to back
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const uint64_t dv = smem_desc(vb + half * kHalfBytes);
-#pragma unroll
-            for (int c = 0; c < kSub / 16; ++c)
-              mma_ts_1(tmem + kColO + x * kV + half * kD, tmem + kColS + x * 128 + hb * kSub + c * 8, desc_advance(dv, c * 2048),
-                       kIdescPV, (u > 0 || c > 0) ? 1u : 0u);
-          }
-        }
-        __syncwarp();
-        if (u >= nsteps - 2) tc_commit(&bar->pv_done[x]);
-        if (hb == 1) {                      // both halves of the V tile are in flight or done
-          tc_commit(&bar->v_empty[sv]);
-          if (++sv == kVS) { sv = 0; phv ^= 1; }
-        }
-        if (more) scores(u + 2);
+      if (h == 0) {
+        ok = warp_wait<kSuspendNs>(&bar->k_full[sk], phk, &bar->abort_flag, p.status);
+        if (!ok) return false;
       }
+      tc_fence_after();
+      const int qb = (qn - 1) & 1;
+      --s_left;
+      if (elect_one()) {
+        const uint64_t dq = dQ0 + (uint64_t)(qb * (kTileBytes >> 4)), dk = dK0 + (uint64_t)(sk * (kTileBytes >> 4));
+#pragma unroll
+        for (int c = 0; c < kD / 16; ++c)
+          mma_ss_1(dS, desc_advance(dq, c * 32), desc_advance(dk, h * (kSub * kD * 2) + c * 32), kIdescQK, c > 0 ? 1u : 0u);
+        commit_1(&bar->s_full[x][h]);
+        if (h == 1) commit_1(&bar->k_empty[sk]);
+        if (s_left == 0) commit_1(&bar->q_empty[qb]);        // the item's last scores: its query tile may be replaced
+      }
+      __syncwarp();
+      if (h == 1 && ++sk == kKS) { sk = 0; phk ^= 1; }
+      return true;
+    };
+    // Product of the next step, of half h of its tile; par: parity of its probabilities' barrier
+    auto next_product = [&](uint32_t h, uint32_t par) {
+      if (v_left == 0) {
+        itv.next(p.items);
+        v_left = 2 * (itv.t1 - itv.t0);
+        v_first = true;
+      }
+      if (h == 0) ok = warp_wait<kSuspendNs>(&bar->v_full[sv], phv, &bar->abort_flag, p.status);
+      if (ok) ok = warp_wait<kSuspendNs>(&bar->p_full[x][h], par, &bar->abort_flag, p.status);
+      if (!ok) return;
+      tc_fence_after();
+      if (elect_one()) {
+        const uint64_t dv = dV0 + (uint64_t)(sv * (kTileBytes >> 4));
+#pragma unroll
+        for (int c = 0; c < kSub / 16; ++c)
+          mma_ts_1(dO, dP + h * 32 + c * 8, desc_advance(dv, h * (kSub * kD * 2) + c * 2048), kIdescPV, c > 0 || !v_first ? 1u : 0u);
+        commit_1(&bar->pv_done[x][h]);
+        if (h == 1) commit_1(&bar->v_empty[sv]);
+      }
+      __syncwarp();
+      v_first = false;
+      --v_left;
+      if (h == 1 && ++sv == kVS) { sv = 0; phv ^= 1; }
+    };
+    bool more = next_scores(0);
+    for (uint32_t g = 0; more && ok; ++g) {           // step g has its scores
+      const uint32_t h = g & 1, par = (g >> 1) & 1;
+      const bool first = g > 0 && v_left == 1;        // step g begins an item: the product before it is an item's last
+      if (first) next_product(h ^ 1, ((g - 1) >> 1) & 1);
+      if (ok) ok = warp_wait<kSuspendNs>(&bar->decided[x][h], par, &bar->abort_flag, p.status);
+      if (!ok) break;
+      more = next_scores(h ^ 1);
+      if (ok && g > 0 && !first) next_product(h ^ 1, ((g - 1) >> 1) & 1);
+      if (ok && !more) next_product(h, par);          // the block's last step
     }
     // Teardown: every MMA issued so far must have retired before tensor memory is released.
     tc_commit(&bar->drain);
@@ -262,108 +292,116 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
       while (!mbar_try(&bar->drain, 0) && globaltimer() - t0 < kWaitLimitNs) {}
     }
     __syncwarp();
-  } else {
-    // ================= softmax + epilogue: one thread per query row and map =================
-    const int x = (warp - kFirstSoftmaxWarp) >> 2;  // map of this warp
+  } else if (warp >= kFirstSoftmaxWarp) {
+    // ================= softmax + epilogue: one thread per query row, map and parity of the step =================
+    const int set = (warp - kFirstSoftmaxWarp) >> 2, x = set >> 1, hb = set & 1;   // map, and parity of the steps, of this warp
     const int q4 = warp & 3;                        // tensor-memory quadrant a warp may touch: warp % 4
     const int r = 32 * q4 + lane;                   // row of the tile
     const uint32_t lane_base = (uint32_t)(q4 << 5) << 16;
-    const uint32_t tS0 = tmem + lane_base + kColS + x * 128;   // score buffer 0 (buffer 1: + 64); probabilities over a buffer's first 32 columns
+    const uint32_t tS = tmem + lane_base + kColS + x * kSub, tP = tmem + lane_base + kColP + 32 * set;
     const uint32_t tO = tmem + lane_base + kColO + x * kV;
     const float sl2 = p.scale_log2;
-    const float kLazy = 8.f / sl2;                 // the reference maximum moves only when it grew by > 2^8
+    const float kLazy = 8.f / sl2;                 // the reference moves only when the maximum grew by > 2^8
     const uint64_t sl2x2 = pack2(sl2, sl2);
-    const float lam = x == 0 ? 1.f : -lambda_of(p.tail);
+    const float lam = lambda_of(p.tail);
     bool ok = true;
-    uint32_t sc = 0;                  // parity of s_full[x][h] in bit h
+    uint32_t n = 0;                   // steps of this set so far: parity of its barriers; the map's other set has done as many before an item
     int vt = 0;                       // V tiles walked so far
-    uint32_t whole = 0;               // items written whole so far: parity of sums_in and read_out
+    uint32_t items = 0;               // items so far: parity of sums_in and read_out
 
     while (ok && it.next(p.items)) {
       const int nsteps = 2 * (it.t1 - it.t0);
       const Reach reach = reach_of(p.items.kv_len, p.items.q_pos, it.ib, p.items.Nq, p.items.Nk, p.items.causal != 0);
       const int i = it.iqt * kTile + r;                                                  // this thread's query
       const int limit = reach.limit(i), limit0 = reach.limit(it.iqt * kTile + 32 * q4);    // its keys; the fewest of the warp
-      // first step of the tile with the last key: rows of V behind it may hold anything, and 0 times that need not be 0
-      const int zero_step = reach.len < min(it.n * kTile, p.items.Nk) && it.t1 == it.n ? nsteps - 2 : -1;
+      // steps of the tile with the last key: rows of V behind it may hold anything, and 0 times that need not be 0
+      const int zero_step = reach.len < min(it.n * kTile, p.items.Nk) && it.t1 == it.n ? nsteps - 2 + hb : -1;
       float m = -INFINITY, l = 0.f;
-      for (int u = 0; u < nsteps; ++u) {
-        const uint32_t tS = tS0 + (u & 1) * kSub;
-        const int key0 = (it.t0 + (u >> 1)) * kTile + (u & 1) * kSub;
-        ok = warp_wait<kSuspendNs>(&bar->s_full[x][u & 1], (sc >> (u & 1)) & 1, &bar->abort_flag, p.status);
+      for (int u = hb; u < nsteps; u += 2, ++n) {
+        const int key0 = (it.t0 + (u >> 1)) * kTile + hb * kSub;
+        ok = warp_wait<kSuspendNs>(&bar->s_full[x][hb], n & 1, &bar->abort_flag, p.status);
         if (!ok) break;
-        sc ^= 1u << (u & 1);
         tc_fence_after();
-        uint32_t va[32], vb2[32];
-        // ---- pass 1: the step's maximum; both halves of the scores stay in registers for pass 2
-        float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        tmem_ld32(tS, va);
-        tmem_ld32(tS + 32, vb2);
-        tmem_wait_ld(va);
-        tmem_wait_ld(vb2);
-        if (key0 + kSub > limit0) {                 // keys that some row of the warp does not see
-          const int nv = limit - key0;
-#pragma unroll
-          for (int c = 0; c < 32; ++c) {
-            if (c >= nv) va[c] = kNegInf;           // exp2(-inf) = 0 and -inf never wins the maximum
-            if (c + 32 >= nv) vb2[c] = kNegInf;
-          }
-        }
+        const bool masked = key0 + kSub > limit0;       // keys that some row of the warp does not see
+        uint32_t va[32], vb[32];
         if (u == zero_step) {
           const int s = (vt + (u >> 1)) % kVS;
           ok = warp_wait<kSuspendNs>(&bar->v_full[s], ((vt + (u >> 1)) / kVS) & 1, &bar->abort_flag, p.status);
           if (!ok) break;
-          if (key0 + r >= reach.len) {              // (both maps' threads write the same zeros: each map's products wait for its own)
-            unsigned char* row = smem + (kQB + kKS + s) * kTileBytes + r * (kD * 2);
+          // this step's half of the tile, both maps' threads the same zeros: each map's products wait for its own
+          const int row = hb * kSub + (r >> 1);
+          if (key0 + (r >> 1) >= reach.len) {
+            unsigned char* dst = smem + (kQB + kKS + s) * kTileBytes + (r & 1) * kHalfBytes + row * (kD * 2);
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
-              *reinterpret_cast<uint4*>(row + 16 * c) = make_uint4(0u, 0u, 0u, 0u);
-              *reinterpret_cast<uint4*>(row + kHalfBytes + 16 * c) = make_uint4(0u, 0u, 0u, 0u);
-            }
+            for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(dst + 16 * c) = make_uint4(0u, 0u, 0u, 0u);
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
+        // ---- pass 1: the step's maximum
+        float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        tmem_ld32(tS, va);
+        tmem_ld32(tS + 32, vb);
+        const float now = bar->ref[x][r];              // the reference as the step before has left it
+        tmem_wait_ld(va);
+        tmem_wait_ld(vb);
+        if (masked) {
+          const int nv = limit - key0;
+#pragma unroll
+          for (int c = 0; c < 32; ++c) {
+            if (c >= nv) va[c] = kNegInf;              // exp2(-inf) = 0 and -inf never wins the maximum
+            if (c + 32 >= nv) vb[c] = kNegInf;
+          }
+        }
         max32(va, mx4);
-        max32(vb2, mx4);
+        max32(vb, mx4);
         const float mx = max_of(mx4);
-        if (u == nsteps - 1) {         // (a key tile is two steps: u > 0)
-          ok = warp_wait<kSuspendNs>(&bar->pv_done[x], 0, &bar->abort_flag, p.status);
-          if (!ok) break;
+        if (u > 0 && now != m) {       // the step before has moved the reference (no number: always)
+          l *= ref_scale(m, now, sl2);
+          m = now;
         }
         float o_scale = 1.f;
-        if (ref_moves(mx, m, kLazy)) { // always true on the first step, unless all of its scores are -inf
-          o_scale = ref_scale(m, mx, sl2);            // first step: 0
+        if (ref_moves(mx, m, kLazy)) { // always on the first step, unless all of its scores are -inf
+          o_scale = ref_scale(m, mx, sl2);              // first step: 0
           l *= o_scale;
           m = mx;
+          bar->ref[x][r] = m;
+        } else if (u == 0) {
+          bar->ref[x][r] = m;
         }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar->decided[x][hb]);
         if (u > 0 && __any_sync(0xffffffffu, o_scale != 1.f)) {
-          // Rare: the reference moved.  O may be touched once the previous step's P V has retired, which the next step's scores
-          // say (a look at their barrier; the next step waits for the same phase); the next P V waits for this step's P.
-          if (u < nsteps - 1) {
-            ok = warp_wait<kSuspendNs>(&bar->s_full[x][(u + 1) & 1], (sc >> ((u + 1) & 1)) & 1, &bar->abort_flag, p.status);
-            if (!ok) break;
-          }
+          // Rare: the reference moved.  O may be touched once the previous step's P V has retired; the next one waits for this step's P.
+          ok = warp_wait<kSuspendNs>(&bar->pv_done[x][hb ^ 1], (n + hb + 1) & 1, &bar->abort_flag, p.status);
+          if (!ok) break;
           tc_fence_after();
 #pragma unroll 1
-          for (int c = 0; c < kV / 32; ++c) {
-            uint32_t v[32];
-            tmem_ld32(tO + 32 * c, v);
-            tmem_wait_ld(v);
+          for (int c = 0; c < kV; c += 8) {    // (few registers: the scores stay where they are)
+            uint32_t v[8];
+            asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
+                         : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(tO + c) : "memory");
 #pragma unroll
-            for (int y = 0; y < 32; ++y) v[y] = __float_as_uint(__uint_as_float(v[y]) * o_scale);
-            tmem_st32(tO + 32 * c, v);
+            for (int y = 0; y < 8; ++y) v[y] = __float_as_uint(__uint_as_float(v[y]) * o_scale);
+            asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                         ::"r"(tO + c), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
           }
           tmem_wait_st();
         }
-        // ---- pass 2: exponentials against the reference, P over the scores just consumed
+        // ---- pass 2: exponentials against the reference
         const float mneg = ref_negative(m, sl2);
         const uint64_t mnegx2 = pack2(mneg, mneg);
         uint64_t lsum[4] = {0ull, 0ull, 0ull, 0ull};
         uint32_t pk[16];
         exp32<false, kPolyOf8, kPolyDeg>(va, sl2x2, mnegx2, lsum, pk, mx4);
-        tmem_st16(tS, pk);
-        exp32<false, kPolyOf8, kPolyDeg>(vb2, sl2x2, mnegx2, lsum, pk, mx4);
-        tmem_st16(tS + 16, pk);
+        if (n > 0) {                   // P(u - 2) has been read
+          ok = warp_wait<kSuspendNs>(&bar->pv_done[x][hb], (n + 1) & 1, &bar->abort_flag, p.status);
+          if (!ok) break;
+          tc_fence_after();
+        }
+        tmem_st16(tP, pk);
+        exp32<false, kPolyOf8, kPolyDeg>(vb, sl2x2, mnegx2, lsum, pk, mx4);
+        tmem_st16(tP + 16, pk);
         float a0, a1, b0, b1;
         unpack2(add2(lsum[0], lsum[1]), a0, a1);
         unpack2(add2(lsum[2], lsum[3]), b0, b1);
@@ -371,73 +409,87 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
         // publish P
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(&bar->p_full[x][u & 1]);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar->p_full[x][hb]);
       }
       if (!ok) break;
       vt += nsteps >> 1;
-      ok = warp_wait<kSuspendNs>(&bar->pv_done[x], 1, &bar->abort_flag, p.status);   // the item's last P V
+      bar->sum[x][hb][r] = l;
+      if (hb == 0) {
+        bar->base[x][r] = m;           // (the last step, the other set's, may still move the reference)
+      } else {                         // the item's last product: the sets of parity 1 wait for it, the others for them
+        ok = warp_wait<kSuspendNs>(&bar->pv_done[x][1], (n + 1) & 1, &bar->abort_flag, p.status);
+        if (!ok) break;
+      }
+      tc_fence_after();
+      tc_fence_before();
+      mbar_arrive(&bar->sums_in);
+      ok = warp_wait<kSuspendNs>(&bar->sums_in, items & 1, &bar->abort_flag, p.status);
       if (!ok) break;
       tc_fence_after();
+      auto total = [&](int map) {
+        const float now = bar->ref[map][r], was = bar->base[map][r], s = bar->sum[map][0][r];
+        return (now != was ? s * ref_scale(was, now, sl2) : s) + bar->sum[map][1][r];
+      };
       if (!it.whole()) {
-        // ---- a part: reference, sum and product of this map as they are
+        // ---- a part: reference, sum and product of this map as they are, half the channels to each set
         float* dst = p.partial + ((size_t)partial_slot(blockIdx.x, it.t0) * kTile + r) * kPartial;
-        *reinterpret_cast<float2*>(dst + 2 * x) = make_float2(m * sl2, l);
-        dst += 4 + kV * x;
+        if (hb == 0) *reinterpret_cast<float2*>(dst + 2 * x) = make_float2(bar->ref[x][r] * sl2, total(x));
+        dst += 4 + kV * x + kD * hb;
 #pragma unroll 1
-        for (int c = 0; c < kV / 32; ++c) {
+        for (int c = 0; c < kD / 32; ++c) {
           uint32_t v[32];
-          tmem_ld32(tO + 32 * c, v);
+          tmem_ld32(tO + kD * hb + 32 * c, v);
           tmem_wait_ld(v);
 #pragma unroll
           for (int y = 0; y < 8; ++y)
             *reinterpret_cast<uint4*>(dst + 32 * c + 4 * y) = make_uint4(v[4 * y], v[4 * y + 1], v[4 * y + 2], v[4 * y + 3]);
         }
         tc_fence_before();
+        mbar_arrive(&bar->read_out);
+        ok = warp_wait<kSuspendNs>(&bar->read_out, items & 1, &bar->abort_flag, p.status);
+        ++items;
         continue;
       }
-      // ---- the whole: x = O_0 / l_0 - lambda O_1 / l_1 on this thread's 64 channels
-      const float mine = lam * ref_inverse(m, l);
-      bar->swap[x][r] = mine;
-      tc_fence_before();
-      mbar_arrive(&bar->sums_in);
-      ok = warp_wait<kSuspendNs>(&bar->sums_in, whole & 1, &bar->abort_flag, p.status);
-      if (!ok) break;
-      tc_fence_after();
-      const float other = bar->swap[x ^ 1][r], f0 = x == 0 ? mine : other, f1 = x == 0 ? other : mine;
-      const uint32_t tX = tmem + lane_base + kColO + x * kD;
-      float out[kD], ss = 0.f;
+      // ---- the whole: x = O_0 / l_0 - lambda O_1 / l_1 on this thread's 32 channels
+      const float f0 = ref_inverse(bar->ref[0][r], total(0));
+      const float f1 = -lam * ref_inverse(bar->ref[1][r], total(1));
+      const uint32_t tX = tmem + lane_base + kColO + 32 * set;
+      float out[32], ss = 0.f;
+      {
+        uint32_t v[32];
+        tmem_ld32(tX, v);
+        tmem_wait_ld(v);
 #pragma unroll
-      for (int c = 0; c < kD / 32; ++c) {
-        uint32_t v0[32], v1[32];
-        tmem_ld32(tX + 32 * c, v0);
-        tmem_ld32(tX + kV + 32 * c, v1);
-        tmem_wait_ld(v0);
-        tmem_wait_ld(v1);
+        for (int y = 0; y < 32; ++y) out[y] = __uint_as_float(v[y]) * f0;
+        tmem_ld32(tX + kV, v);
+        tmem_wait_ld(v);
 #pragma unroll
         for (int y = 0; y < 32; ++y) {
-          const float d = fmaf(__uint_as_float(v0[y]), f0, __uint_as_float(v1[y]) * f1);
-          out[32 * c + y] = limit > 0 ? d : 0.f;    // a row that sees no key
-          ss = fmaf(out[32 * c + y], out[32 * c + y], ss);
+          const float d = fmaf(__uint_as_float(v[y]), f1, out[y]);
+          out[y] = limit > 0 ? d : 0.f;             // a row that sees no key
+          ss = fmaf(out[y], out[y], ss);
         }
       }
-      bar->swap[x ^ 1][r] = ss;                     // (the place that this thread has just read, and nobody else does)
+      bar->square[set][r] = ss;
       tc_fence_before();
       mbar_arrive(&bar->read_out);
-      ok = warp_wait<kSuspendNs>(&bar->read_out, whole & 1, &bar->abort_flag, p.status);
+      ok = warp_wait<kSuspendNs>(&bar->read_out, items & 1, &bar->abort_flag, p.status);
       if (!ok) break;
       tc_fence_after();
-      ++whole;
+      ++items;
       float rn = 1.f;
       if (p.tail.norm_w)
-        rn = (1.f - p.tail.lambda_init) * rsqrtf((x == 0 ? ss + bar->swap[x][r] : bar->swap[x][r] + ss) * (1.f / kV) + p.tail.norm_eps);
+        rn = (1.f - p.tail.lambda_init) *
+             rsqrtf(((bar->square[0][r] + bar->square[1][r]) + (bar->square[2][r] + bar->square[3][r])) * (1.f / kV) + p.tail.norm_eps);
       if (i < p.items.Nq) {
-        __nv_bfloat16* dst = p.o + (((size_t)it.ib * 2 * p.pairs + 2 * it.ipair + x) * p.items.Nq + i) * kD;
+        __nv_bfloat16* dst = p.o + (((size_t)it.ib * 2 * p.pairs + 2 * it.ipair + x) * p.items.Nq + i) * kD + 32 * hb;
 #pragma unroll
-        for (int c = 0; c < kD / 8; ++c) {
+        for (int c = 0; c < 4; ++c) {
           float w[8];
 #pragma unroll
           for (int y = 0; y < 8; y += 4) {
-            const float4 g = p.tail.norm_w ? __ldg(reinterpret_cast<const float4*>(p.tail.norm_w + kD * x + 8 * c + y)) : make_float4(1.f, 1.f, 1.f, 1.f);
+            const float4 g = p.tail.norm_w ? __ldg(reinterpret_cast<const float4*>(p.tail.norm_w + 32 * set + 8 * c + y)) : make_float4(1.f, 1.f, 1.f, 1.f);
             w[y] = g.x; w[y + 1] = g.y; w[y + 2] = g.z; w[y + 3] = g.w;
           }
           uint32_t pk[4];
@@ -572,6 +624,10 @@ cudaError_t launch_diff_tc(const DiffArgs& a, void* ws, int* status, cudaStream_
   }
   static OncePerDevice smem_opt_in;   // > 48 KB of dynamic shared memory: a per-device function attribute
   cudaError_t e = smem_opt_in.run([] {
+    cudaFuncAttributes attr;       // the split of the registers counts on those that a block is launched with
+    const cudaError_t r = cudaFuncGetAttributes(&attr, attn_diff_kernel);
+    if (r != cudaSuccess) return r;
+    if (attr.numRegs * kThreads < 128 * kRegsRoles + 512 * kRegsSoftmax) return cudaErrorInvalidConfiguration;
     return cudaFuncSetAttribute(attn_diff_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
   });
   if (e != cudaSuccess) return e;
