@@ -523,7 +523,11 @@ jv_status jv_layer_norm_grad(const void* dy, const void* x, const float* w, cons
 size_t jv_diff_attn_workspace_bytes(const jv_diff_shape* shape) {
   InStrides qs, ks;
   if (check_diff(shape, &qs, &ks) != JV_OK) return 0;
-  return diff_workspace_bytes(shape->B, shape->H / 2, shape->Hkv / 2, shape->Nq, shape->Nk, shape->D, shape->dtype, shape->causal != 0);
+  if (shape->dtype != JV_BF16 || shape->D != 64) return 0;                // (the fp32 kernel needs none)
+  const int pairs = shape->H / 2, kv_pairs = shape->Hkv / 2;
+  const size_t tiles = diff_tc_plan(shape->B, pairs, shape->Nq, shape->Nk, shape->causal != 0).total;
+  const size_t rows = diff_rows_plan(shape->B, kv_pairs, shape->Nk).total;
+  return (int64_t)(pairs / kv_pairs) * shape->Nq <= 16 ? rows : tiles;
 }
 
 jv_status jv_diff_attn(const void* q, const void* k, const void* v, void* o, const jv_diff_shape* shape, const jv_diff* diff,
@@ -548,7 +552,8 @@ jv_status jv_diff_attn(const void* q, const void* k, const void* v, void* o, con
   if (!g_force_generic.load() && diff_tc_supported(a)) {
     int* status = device_status_ptr();
     if (!status) return JV_ERR_CUDA;
-    return from_cuda(launch_diff_tc(a, ws, status, (cudaStream_t)cuda_stream));
+    return from_cuda(diff_rows_supported(a) ? launch_diff_rows(a, ws, status, (cudaStream_t)cuda_stream)
+                                            : launch_diff_tc(a, ws, status, (cudaStream_t)cuda_stream));
   }
   return from_cuda(launch_diff_generic(a, (cudaStream_t)cuda_stream));
 }
