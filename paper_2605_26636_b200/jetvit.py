@@ -435,51 +435,85 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-def _f32_on(t: Optional[torch.Tensor], shape, device, what: str):
-    """``t`` (or None) has to be a contiguous fp32 tensor of that shape on the call's device."""
-    if t is not None and not (t.is_cuda and t.device == device and t.dtype == torch.float32 and t.is_contiguous()
-                              and tuple(t.shape) == tuple(shape)):
-        raise ValueError(f"{what} must be a contiguous fp32 CUDA tensor of {list(shape)} on the call's device")
+# The calls from here on are used token by token, where the checks of their arguments would take longer than their kernels: they
+# look at each attribute once, and at the device by its index (-1: not a CUDA tensor).
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
+
+
+def _index(t: torch.Tensor) -> int:
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError("tensors must live on a CUDA device (there is no CPU path)")
+    return dev
+
+
+def _like(t: Optional[torch.Tensor], shape, dtype, dev: int, what: str):
+    """``t`` (or None) has to be a contiguous tensor of that shape and type on the call's device."""
+    if t is not None and not (t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous()):
+        raise ValueError(f"{what} must be a contiguous {dtype} CUDA tensor of {list(shape)} on the call's device")
+
+
+def _per_row(t: Optional[torch.Tensor], n: int, dtype, dev: int, what: str):
+    if t is None or not (t.dtype is dtype and t.numel() == n and t.get_device() == dev and t.is_contiguous()):
+        raise ValueError(f"{what} must be a contiguous {dtype} CUDA tensor of {n} elements on the call's device")
+
+
+def _enqueue(dev: int, stream, call):
+    """call(stream handle) with the tensors' device current."""
+    if dev == _get_device():
+        return call(stream.cuda_stream if stream is not None else _raw_stream(dev) if _raw_stream is not None else _stream(None))
+    with torch.cuda.device(dev):
+        return call(_stream(stream))
+
+
+def _scratch(n: int, device, stream) -> Optional[torch.Tensor]:
+    if n == 0:
+        return None
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    if stream is not None:
+        ws.record_stream(stream)          # freed by torch on the current stream, used on `stream`
+    return ws
 
 
 def _rows(t: torch.Tensor, what: str):
     """(rows, C, elements between rows) of a [..., C] tensor whose rows lie evenly spaced."""
-    if not t.is_cuda:
-        raise ValueError("tensors must live on a CUDA device (there is no CPU path)")
-    if t.dim() < 1 or t.numel() == 0:
+    n = t.numel()
+    if n == 0 or t.dim() < 1:
         raise ValueError(f"{what} must be a [..., C] tensor that is not empty")
     C = t.shape[-1]
     if t.is_contiguous():
-        return t.numel() // C, C, C
+        return n // C, C, 0
     try:
         flat = t.view(-1, C)
     except RuntimeError:
         flat = None
     if flat is None or (C > 1 and flat.stride(1) != 1) or (flat.shape[0] > 1 and flat.stride(0) < C):
         raise ValueError(f"the rows of {what} must be contiguous, evenly spaced and apart from each other")
-    return flat.shape[0], C, flat.stride(0) if flat.shape[0] > 1 else C
+    return flat.shape[0], C, flat.stride(0) if flat.shape[0] > 1 else 0
 
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-6, out=None, stats=None, stream=None) -> torch.Tensor:
     """jv_layer_norm over the last axis of ``x`` (f32 or bf16, [..., C]; rows evenly spaced); ``weight`` and ``bias`` fp32 [C] or
     None.  ``stats``: an optional pair of fp32 tensors of one element per row that receive mean and 1 / standard
     deviation, which layer_norm_grad takes."""
+    dev = _index(x)
     rows, C, stride = _rows(x, "x")
-    shape = JvNormShape(rows, C, _dtype_code(x), stride, 0)
-    _f32_on(weight, (C,), x.device, "weight")
-    _f32_on(bias, (C,), x.device, "bias")
-    mean, rstd = stats if stats is not None else (None, None)
+    vec = (C,)
+    _like(weight, vec, _F32, dev, "weight")
+    _like(bias, vec, _F32, dev, "bias")
+    mean = rstd = None
     if stats is not None:
-        for t in (mean, rstd):
-            if t.numel() != rows:
-                raise ValueError("stats must hold one element per row")
-            _f32_on(t, t.shape, x.device, "stats")
-    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-    if not (out.is_cuda and out.is_contiguous() and out.shape == x.shape and out.dtype == x.dtype and out.device == x.device):
-        raise ValueError("out must be a contiguous tensor of x's shape, dtype and device")
-    with _current_device(x.device):
-        st = lib().jv_layer_norm(x.data_ptr(), _ptr(weight), _ptr(bias), out.data_ptr(), _ptr(mean), _ptr(rstd),
-                                 ctypes.byref(shape), float(eps), _stream(stream))
+        mean, rstd = stats
+        _per_row(mean, rows, _F32, dev, "stats")
+        _per_row(rstd, rows, _F32, dev, "stats")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _like(out, x.shape, x.dtype, dev, "out")
+    shape = JvNormShape(rows, C, _dtype_code(x), stride)
+    st = _enqueue(dev, stream, lambda s: lib().jv_layer_norm(
+        x.data_ptr(), _ptr(weight), _ptr(bias), out.data_ptr(), _ptr(mean), _ptr(rstd), ctypes.byref(shape), eps, s))
     _raise(st, "jv_layer_norm")
     return out
 
@@ -488,51 +522,47 @@ def layer_norm_grad(dy, x, weight, mean, rstd, weight_grad: bool = True, bias_gr
                     ws: Optional[torch.Tensor] = None, stream=None):
     """jv_layer_norm_grad: (dx, dw, db) of layer_norm from ``dy`` and what the forward pass left in ``stats``.  dw and db are fp32
     [C], None where not wanted.  ``out``: an optional (dx, dw, db) to write into."""
+    dev = _index(x)
     rows, C, stride = _rows(x, "x")
-    if dy.shape != x.shape or dy.dtype != x.dtype or dy.device != x.device:
+    if dy.shape != x.shape or dy.dtype is not x.dtype or dy.get_device() != dev:
         raise ValueError("dy must have x's shape, dtype and device")
-    shape = JvNormShape(rows, C, _dtype_code(x), stride, _rows(dy, "dy")[2])
-    _f32_on(weight, (C,), x.device, "weight")
-    for t in (mean, rstd):
-        if t is None or t.numel() != rows:
-            raise ValueError("mean and rstd must hold one element per row")
-        _f32_on(t, t.shape, x.device, "mean and rstd")
+    vec = (C,)
+    _like(weight, vec, _F32, dev, "weight")
+    _per_row(mean, rows, _F32, dev, "mean")
+    _per_row(rstd, rows, _F32, dev, "rstd")
     if out is None:
-        new = lambda want: torch.empty(C, dtype=torch.float32, device=x.device) if want else None
-        out = (torch.empty(x.shape, dtype=x.dtype, device=x.device), new(weight_grad), new(bias_grad))
-    dx, dw, db = out
-    if not (dx.is_cuda and dx.is_contiguous() and dx.shape == x.shape and dx.dtype == x.dtype and dx.device == x.device):
-        raise ValueError("dx must be a contiguous tensor of x's shape, dtype and device")
-    _f32_on(dw, (C,), x.device, "dw")
-    _f32_on(db, (C,), x.device, "db")
-    with _current_device(x.device):
-        if ws is None and (dw is not None or db is not None):
-            ws = torch.empty(int(lib().jv_layer_norm_grad_workspace_bytes(ctypes.byref(shape))), dtype=torch.uint8, device=x.device)
-            if stream is not None:
-                ws.record_stream(stream)
-        wp, wn = _ws_args(ws)
-        st = lib().jv_layer_norm_grad(dy.data_ptr(), x.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(),
-                                      _ptr(dw), _ptr(db), ctypes.byref(shape), wp, wn, _stream(stream))
-    _raise(st, "jv_layer_norm_grad")
+        new = lambda want: torch.empty(C, dtype=_F32, device=x.device) if want else None
+        dx, dw, db = out = (torch.empty(x.shape, dtype=x.dtype, device=x.device), new(weight_grad), new(bias_grad))
+    else:
+        dx, dw, db = out
+        _like(dx, x.shape, x.dtype, dev, "dx")
+        _like(dw, vec, _F32, dev, "dw")
+        _like(db, vec, _F32, dev, "db")
+    shape = JvNormShape(rows, C, _dtype_code(x), stride, _rows(dy, "dy")[2])
+
+    def call(s):
+        scratch = ws
+        if scratch is None and (dw is not None or db is not None):
+            scratch = _scratch(int(lib().jv_layer_norm_grad_workspace_bytes(ctypes.byref(shape))), x.device, stream)
+        wp, wn = _ws_args(scratch)
+        return lib().jv_layer_norm_grad(dy.data_ptr(), x.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(),
+                                        _ptr(dw), _ptr(db), ctypes.byref(shape), wp, wn, s)
+
+    _raise(_enqueue(dev, stream, call), "jv_layer_norm_grad")
     return dx, dw, db
 
 
-def _i32_on(t: Optional[torch.Tensor], n: int, device, what: str):
-    if t is not None and not (t.is_cuda and t.device == device and t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n):
-        raise ValueError(f"{what} must be a contiguous int32 CUDA tensor of {n} elements on the call's device")
-
-
 def _head_strides(t: torch.Tensor, what: str):
-    """Elements between {tokens, heads, batch elements} of a [B, H, N, D] tensor; zeros where it is contiguous."""
+    """Elements between {tokens, heads, batch elements} of a [B, H, N, D] tensor; None where it is contiguous."""
     if t.is_contiguous():
-        return 0, 0, 0
+        return None
     B, H, N, D = t.shape
     sb, sh, sn, sd = t.stride()
     if sd != 1 and D > 1:
         raise ValueError(f"the channels of {what} must be contiguous")
-    e = max(1, 16 // t.element_size())                 # where there is one of something, any step does
-    sn, sh, sb = (s if n > 1 else max(D, e) for n, s in ((N, sn), (H, sh), (B, sb)))
-    if min(sn, sh, sb) <= 0:
+    e = max(D, 16 // t.element_size())                 # where there is one of something, any step does
+    sn, sh, sb = sn if N > 1 else e, sh if H > 1 else e, sb if B > 1 else e
+    if sn <= 0 or sh <= 0 or sb <= 0:
         raise ValueError(f"{what} must not repeat its rows")
     return sn, sh, sb
 
@@ -541,51 +571,51 @@ def diff_attn(q, k, v, lam, lambda_init: float, norm_weight=None, norm_eps: floa
               q_pos=None, scale: float = 0.0, out=None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """jv_diff_attn: q [B, H, Nq, D], k and v [B, Hkv, Nk, D], heads in pairs; any strides with contiguous channels, k and v
     alike.  ``lam``: the four learned vectors, fp32 [4, D]; ``norm_weight``: fp32 [2 D] or None; ``kv_len``, ``q_pos``: int32 [B] or None."""
-    if q.dim() != 4 or k.dim() != 4 or k.shape != v.shape or q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3]:
+    dev, dtype, qs, kvs = _index(q), q.dtype, q.shape, k.shape
+    if len(qs) != 4 or len(kvs) != 4 or v.shape != kvs or qs[0] != kvs[0] or qs[3] != kvs[3]:
         raise ValueError("q must be [B, H, Nq, D], k and v [B, Hkv, Nk, D]")
-    for t in (q, k, v):
-        if not t.is_cuda:
-            raise ValueError("tensors must live on a CUDA device (there is no CPU path)")
-        if t.dtype != q.dtype or t.device != q.device:
-            raise ValueError("q, k and v must have one dtype and device")
-    B, H, Nq, D = q.shape
-    Hkv, Nk = k.shape[1], k.shape[2]
-    ks = _head_strides(k, "k")
-    if _head_strides(v, "v") != ks:
+    if k.dtype is not dtype or v.dtype is not dtype or k.get_device() != dev or v.get_device() != dev:
+        raise ValueError("q, k and v must have one dtype and device")
+    B, H, Nq, D = qs
+    shape = JvDiffShape(B, H, kvs[1], Nq, kvs[2], D, _dtype_code(q), 1 if causal else 0)
+    strides = _head_strides(k, "k")
+    if _head_strides(v, "v") != strides:
         raise ValueError("k and v must have the same strides")
-    _f32_on(lam, (4, D), q.device, "lam")
-    _f32_on(norm_weight, (2 * D,), q.device, "norm_weight")
-    _i32_on(kv_len, B, q.device, "kv_len")
-    _i32_on(q_pos, B, q.device, "q_pos")
-    shape = JvDiffShape(B, H, Hkv, Nq, Nk, D, _dtype_code(q), 1 if causal else 0, _head_strides(q, "q"), ks)
+    if strides is not None:
+        shape.kv_stride = strides
+    strides = _head_strides(q, "q")
+    if strides is not None:
+        shape.q_stride = strides
+    _like(lam, (4, D), _F32, dev, "lam")
+    _like(norm_weight, (2 * D,), _F32, dev, "norm_weight")
+    if kv_len is not None:
+        _per_row(kv_len, B, _I32, dev, "kv_len")
+    if q_pos is not None:
+        _per_row(q_pos, B, _I32, dev, "q_pos")
     d = JvDiff(lam.data_ptr(), lambda_init, _ptr(norm_weight), norm_eps, _ptr(kv_len), _ptr(q_pos))
-    out = _empty_out(q) if out is None else out
-    if not (out.is_cuda and out.is_contiguous() and out.shape == q.shape and out.dtype == q.dtype and out.device == q.device):
-        raise ValueError("out must be a contiguous tensor of q's shape, dtype and device")
-    with _current_device(q.device):
-        if ws is None:
-            n = int(lib().jv_diff_attn_workspace_bytes(ctypes.byref(shape)))
-            if n:
-                ws = torch.empty(n, dtype=torch.uint8, device=q.device)
-                if stream is not None:
-                    ws.record_stream(stream)
-        wp, wn = _ws_args(ws)
-        st = lib().jv_diff_attn(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), ctypes.byref(shape), ctypes.byref(d),
-                                float(scale), wp, wn, _stream(stream))
-    _raise(st, "jv_diff_attn")
+    if out is None:
+        out = torch.empty(qs, dtype=dtype, device=q.device)
+    else:
+        _like(out, qs, dtype, dev, "out")
+
+    def call(s):
+        L = lib()
+        scratch = _scratch(L.jv_diff_attn_workspace_bytes(ctypes.byref(shape)), q.device, stream) if ws is None else ws
+        wp, wn = _ws_args(scratch)
+        return L.jv_diff_attn(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), ctypes.byref(shape), ctypes.byref(d),
+                              scale, wp, wn, s)
+
+    _raise(_enqueue(dev, stream, call), "jv_diff_attn")
     return out
 
 
-def _token_rows(t: Optional[torch.Tensor], B: int, L: int, C: int, like: torch.Tensor, what: str):
-    """Elements between {token rows, batch elements} of a [B, L, C] tensor (zeros: contiguous, or no tensor)."""
-    if t is None:
-        return 0, 0
-    if not t.is_cuda:
-        raise ValueError("tensors must live on a CUDA device (there is no CPU path)")
-    if tuple(t.shape) != (B, L, C) or t.dtype != like.dtype or t.device != like.device:
-        raise ValueError(f"{what} must be [{B}, {L}, {C}], of one dtype and device with the others")
+def _token_rows(t: torch.Tensor, shape, dtype, dev: int, what: str):
+    """Elements between {token rows, batch elements} of a [B, L, C] tensor; None where it is contiguous."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{what} must be {list(shape)}, of one dtype and device with the others")
     if t.is_contiguous():
-        return 0, 0
+        return None
+    B, L, C = shape
     sb, sl, sc = t.stride()
     row = sl if L > 1 else C
     batch = sb if B > 1 else L * row
@@ -594,32 +624,32 @@ def _token_rows(t: Optional[torch.Tensor], B: int, L: int, C: int, like: torch.T
     return row, batch
 
 
-def _same(t: Optional[torch.Tensor], shape, like: torch.Tensor, what: str):
-    if t is not None and not (t.is_cuda and t.is_contiguous() and tuple(t.shape) == tuple(shape) and t.dtype == like.dtype
-                              and t.device == like.device):
-        raise ValueError(f"{what} must be a contiguous {list(shape)} tensor of the inputs' dtype and device")
-
-
 def causal_conv(x, weight, bias=None, state=None, state_out=None, lens=None, silu: bool = True, out=None, stream=None) -> torch.Tensor:
     """jv_causal_conv: x [B, L, C] (token rows evenly spaced), ``weight`` fp32 [C, K], ``bias`` fp32 [C] or None; ``state`` (in) and
     ``state_out`` (may be the same tensor) [B, K - 1, C] of x's dtype; ``lens`` int32 [B].  Rows of ``out`` behind a sequence stay as
     they are (so pass one where that matters)."""
-    if x.dim() != 3 or weight.dim() != 2:
+    dev, dtype, xs = _index(x), x.dtype, x.shape
+    if len(xs) != 3 or weight.dim() != 2:
         raise ValueError("x must be [B, L, C] and weight [C, K]")
-    B, L, C = x.shape
+    B, L, C = xs
     K = weight.shape[1]
-    stride = _token_rows(x, B, L, C, x, "x")
-    _f32_on(weight, (C, K), x.device, "weight")
-    _f32_on(bias, (C,), x.device, "bias")
-    _same(state, (B, K - 1, C), x, "state")
-    _same(state_out, (B, K - 1, C), x, "state_out")
-    _i32_on(lens, B, x.device, "lens")
-    out = torch.empty((B, L, C), dtype=x.dtype, device=x.device) if out is None else out
-    _same(out, (B, L, C), x, "out")
-    shape = JvConvShape(B, L, C, K, _dtype_code(x), 1 if silu else 0, stride)
-    with _current_device(x.device):
-        st = lib().jv_causal_conv(x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(state), out.data_ptr(), _ptr(state_out), _ptr(lens),
-                                  ctypes.byref(shape), _stream(stream))
+    shape = JvConvShape(B, L, C, K, _dtype_code(x), 1 if silu else 0)
+    strides = _token_rows(x, xs, dtype, dev, "x")
+    if strides is not None:
+        shape.x_stride = strides
+    _like(weight, (C, K), _F32, dev, "weight")
+    _like(bias, (C,), _F32, dev, "bias")
+    _like(state, (B, K - 1, C), dtype, dev, "state")
+    if state_out is not state:
+        _like(state_out, (B, K - 1, C), dtype, dev, "state_out")
+    if lens is not None:
+        _per_row(lens, B, _I32, dev, "lens")
+    if out is None:
+        out = torch.empty(xs, dtype=dtype, device=x.device)
+    else:
+        _like(out, xs, dtype, dev, "out")
+    st = _enqueue(dev, stream, lambda s: lib().jv_causal_conv(
+        x.data_ptr(), weight.data_ptr(), _ptr(bias), _ptr(state), out.data_ptr(), _ptr(state_out), _ptr(lens), ctypes.byref(shape), s))
     _raise(st, "jv_causal_conv")
     return out
 
@@ -629,31 +659,42 @@ def selective_scan(u, dt, A, Bm, Cm, D=None, z=None, dt_bias=None, state=None, s
     """jv_selective_scan: u, dt, z [B, L, C], Bm, Cm [B, L, Ns] (token rows evenly spaced), A fp32 [C, Ns], D and dt_bias fp32 [C] or None;
     ``state`` (in) and ``state_out`` (may be the same tensor) fp32 [B, C, Ns]; ``lens`` int32 [B].  Rows of ``out`` behind a sequence
     stay as they are."""
-    if u.dim() != 3 or A.dim() != 2:
+    dev, dtype, us = _index(u), u.dtype, u.shape
+    if len(us) != 3 or A.dim() != 2:
         raise ValueError("u must be [B, L, C] and A [C, Ns]")
-    B, L, C = u.shape
+    B, L, C = us
     Ns = A.shape[1]
-    strides = [_token_rows(t, B, L, n, u, what) for t, n, what in ((u, C, "u"), (dt, C, "dt"), (Bm, Ns, "Bm"), (Cm, Ns, "Cm"), (z, C, "z"))]
-    _f32_on(A, (C, Ns), u.device, "A")
-    _f32_on(D, (C,), u.device, "D")
-    _f32_on(dt_bias, (C,), u.device, "dt_bias")
-    _f32_on(state, (B, C, Ns), u.device, "state")
-    _f32_on(state_out, (B, C, Ns), u.device, "state_out")
-    _i32_on(lens, B, u.device, "lens")
-    out = torch.empty((B, L, C), dtype=u.dtype, device=u.device) if out is None else out
-    _same(out, (B, L, C), u, "out")
-    shape = JvScanShape(B, L, C, Ns, _dtype_code(u), 1 if softplus else 0, *strides)
-    with _current_device(u.device):
-        if ws is None:
-            n = int(lib().jv_selective_scan_workspace_bytes(ctypes.byref(shape)))
-            if n:
-                ws = torch.empty(n, dtype=torch.uint8, device=u.device)
-                if stream is not None:
-                    ws.record_stream(stream)
-        wp, wn = _ws_args(ws)
-        st = lib().jv_selective_scan(u.data_ptr(), dt.data_ptr(), A.data_ptr(), Bm.data_ptr(), Cm.data_ptr(), _ptr(D), _ptr(z), _ptr(dt_bias),
-                                     _ptr(state), out.data_ptr(), _ptr(state_out), _ptr(lens), ctypes.byref(shape), wp, wn, _stream(stream))
-    _raise(st, "jv_selective_scan")
+    bs, vec, hs = (B, L, Ns), (C,), (B, C, Ns)
+    shape = JvScanShape(B, L, C, Ns, _dtype_code(u), 1 if softplus else 0)
+    for field, t, want in (("u_stride", u, us), ("dt_stride", dt, us), ("b_stride", Bm, bs), ("c_stride", Cm, bs), ("z_stride", z, us)):
+        if t is not None or field != "z_stride":
+            strides = _token_rows(t, want, dtype, dev, field[:-7])
+            if strides is not None:
+                setattr(shape, field, strides)
+    _like(A, (C, Ns), _F32, dev, "A")
+    _like(D, vec, _F32, dev, "D")
+    _like(dt_bias, vec, _F32, dev, "dt_bias")
+    _like(state, hs, _F32, dev, "state")
+    if state_out is not state:
+        _like(state_out, hs, _F32, dev, "state_out")
+    if lens is not None:
+        _per_row(lens, B, _I32, dev, "lens")
+    if out is None:
+        out = torch.empty(us, dtype=dtype, device=u.device)
+    else:
+        _like(out, us, dtype, dev, "out")
+
+    def call(s):
+        lb = lib()
+        scratch = ws
+        if scratch is None and L > 1:                  # (single tokens need none)
+            scratch = _scratch(lb.jv_selective_scan_workspace_bytes(ctypes.byref(shape)), u.device, stream)
+        wp, wn = _ws_args(scratch)
+        return lb.jv_selective_scan(u.data_ptr(), dt.data_ptr(), A.data_ptr(), Bm.data_ptr(), Cm.data_ptr(), _ptr(D), _ptr(z),
+                                    _ptr(dt_bias), _ptr(state), out.data_ptr(), _ptr(state_out), _ptr(lens), ctypes.byref(shape),
+                                    wp, wn, s)
+
+    _raise(_enqueue(dev, stream, call), "jv_selective_scan")
     return out
 
 
