@@ -11,6 +11,7 @@
 // warp walks, the warps of a block add theirs through shared memory, the blocks' partials go to the workspace and a second
 // launch adds them up, all in a fixed order: no atomics, results repeat bit for bit.
 #include "common.cuh"
+#include "tc_common.cuh"   // packed fp32 arithmetic
 
 namespace jv {
 namespace {
@@ -102,69 +103,222 @@ struct NormParams {
   float eps;
 };
 
-// Columns of lane `tl` (of `nl` that share a row): pieces tl, tl + nl, ...
-template <typename T, int VEC, int NCH, bool BLOCK>
+// Columns of lane `tl` (of `nl` that share a row): pieces tl, tl + nl, ...  R rows of a warp at a time: w and b pass through L1 once for
+// them (for one row of bf16 values they are four times the row's bytes).
+template <typename T, int VEC, int NCH, bool BLOCK, int R>
 __global__ void __launch_bounds__(BLOCK ? 512 : 128, 1) layer_norm_kernel(const NormParams p) {
   __shared__ float red[64];
   griddep_wait();
   griddep_launch_dependents();
   const int tl = BLOCK ? threadIdx.x : threadIdx.x & 31, nl = BLOCK ? blockDim.x : 32;
-  const int64_t row = BLOCK ? blockIdx.x : (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-  if (row >= p.rows) return;        // (whole warps or blocks)
-  const T* x = (const T*)p.x + row * p.x_stride;
-  Piece<T, VEC> in[NCH];
+  const int64_t row0 = BLOCK ? blockIdx.x : ((int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) * R;
+  if (row0 >= p.rows) return;        // (whole warps or blocks)
+  Piece<T, VEC> in[R][NCH];
 #pragma unroll
-  for (int j = 0; j < NCH; ++j) {
-    const int c = (j * nl + tl) * VEC;
-    if (c < p.C) in[j].load(x + c);
+  for (int r = 0; r < R; ++r) {
+    const T* x = (const T*)p.x + min(row0 + r, p.rows - 1) * p.x_stride;
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+      const int c = (j * nl + tl) * VEC;
+      if (c < p.C) in[r][j].load(x + c);
+    }
   }
   const float inv_c = 1.f / (float)p.C;
   int turn = 0;
-  float s[1] = {0.f};
+  float mean[R], rstd[R], s[R];
 #pragma unroll
-  for (int j = 0; j < NCH; ++j)
-    if ((j * nl + tl) * VEC < p.C) {
-      float f[VEC];
-      in[j].get(f);
+  for (int r = 0; r < R; ++r) {
+    s[r] = 0.f;
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) s[0] += f[i];
-    }
-  row_sums<BLOCK, 1>(s, red, turn);
-  const float mean = s[0] * inv_c;
-  s[0] = 0.f;
+    for (int j = 0; j < NCH; ++j)
+      if ((j * nl + tl) * VEC < p.C) {
+        float f[VEC];
+        in[r][j].get(f);
 #pragma unroll
-  for (int j = 0; j < NCH; ++j)
-    if ((j * nl + tl) * VEC < p.C) {
-      float f[VEC];
-      in[j].get(f);
+        for (int i = 0; i < VEC; ++i) s[r] += f[i];
+      }
+  }
+  row_sums<BLOCK, R>(s, red, turn);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) s[0] = fmaf(f[i] - mean, f[i] - mean, s[0]);
-    }
-  row_sums<BLOCK, 1>(s, red, turn);
-  const float rstd = rsqrtf(fmaf(s[0], inv_c, p.eps));
-  T* y = (T*)p.y + row * p.C;
+  for (int r = 0; r < R; ++r) {
+    mean[r] = s[r] * inv_c;
+    s[r] = 0.f;
+#pragma unroll
+    for (int j = 0; j < NCH; ++j)
+      if ((j * nl + tl) * VEC < p.C) {
+        float f[VEC];
+        in[r][j].get(f);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) s[r] = fmaf(f[i] - mean[r], f[i] - mean[r], s[r]);
+      }
+  }
+  row_sums<BLOCK, R>(s, red, turn);
+#pragma unroll
+  for (int r = 0; r < R; ++r) rstd[r] = rsqrtf(fmaf(s[r], inv_c, p.eps));
 #pragma unroll
   for (int j = 0; j < NCH; ++j) {
     const int c = (j * nl + tl) * VEC;
     if (c < p.C) {
-      float f[VEC], w[VEC], b[VEC];
-      in[j].get(f);
+      float w[VEC], b[VEC];
 #pragma unroll
       for (int i = 0; i < VEC; ++i) { w[i] = 1.f; b[i] = 0.f; }
       if (p.w) load_f32<VEC>(p.w + c, w);
       if (p.b) load_f32<VEC>(p.b + c, b);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) f[i] = fmaf((f[i] - mean) * rstd, w[i], b[i]);
-      in[j].set(f);
-      in[j].store(y + c);
+      for (int r = 0; r < R; ++r) {
+        float f[VEC];
+        in[r][j].get(f);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) f[i] = fmaf((f[i] - mean[r]) * rstd[r], w[i], b[i]);
+        in[r][j].set(f);
+        if (R == 1 || row0 + r < p.rows) in[r][j].store((T*)p.y + (row0 + r) * p.C + c);
+      }
     }
   }
-  if (p.mean && tl == 0) {
-    p.mean[row] = mean;
-    p.rstd[row] = rstd;
+  if (p.mean && tl == 0)
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (row0 + r < p.rows) {
+        p.mean[row0 + r] = mean[r];
+        p.rstd[row0 + r] = rstd[r];
+      }
+}
+
+// stages of a warp's ring: 1 KB for a piece of x and dy each
+template <int NCH>
+constexpr int kGradStages = 16 / NCH < 2 ? 2 : 16 / NCH > 4 ? 4 : 16 / NCH;
+
+// ---- gradient, rows of a warp in 16-byte pieces --------------------------------------------------------------------------
+// The rows ahead are on their way into shared memory (cp.async: every lane copies the pieces that it will read, so no barrier
+// is in it) while this one is worked on, twice, from there: registers hold the sums of dw and db and the weights only.
+// One block of twelve warps per SM: few partials, and a ring of 16 KB at most to each warp.
+constexpr int kGradWarps = 12;
+template <typename T, int VEC, int NCH>
+__global__ void __launch_bounds__(kGradWarps * 32, 1) layer_norm_grad_rows_kernel(const NormParams p) {
+  constexpr int kStages = kGradStages<NCH>, kRing = kStages * 2 * NCH * 512;
+  extern __shared__ __align__(16) unsigned char ring[];   // [warp][stage][x, dy][piece][lane] of 16 bytes; at the end [warp][dw, db][columns]
+  griddep_wait();
+  griddep_launch_dependents();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nwarps = blockDim.x >> 5;
+  const int64_t first = (int64_t)blockIdx.x * nwarps + warp, step = (int64_t)gridDim.x * nwarps;
+  unsigned char* mine = ring + (size_t)warp * kRing + lane * 16;
+  auto fetch = [&](int64_t row, int stage) {
+    if (row < p.rows) {
+      const T *x = (const T*)p.x + row * p.x_stride, *dy = (const T*)p.dy + row * p.dy_stride;
+#pragma unroll
+      for (int j = 0; j < NCH; ++j) {
+        const int c = (j * 32 + lane) * VEC;
+        if (c < p.C) {
+          const uint32_t dst = (uint32_t)__cvta_generic_to_shared(mine + (stage * 2 * NCH + j) * 512);
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(x + c) : "memory");
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + NCH * 512), "l"(dy + c) : "memory");
+        }
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // Pairs of values in the packed arithmetic of sm_100: with single values the instructions of a row of bf16, not its bytes, bounded
+  // this (32768 rows of 1024: 50 us).
+  using namespace tc;
+  constexpr int kPairs = VEC / 2;
+  uint64_t dw[NCH][kPairs], db[NCH][kPairs], w[NCH][kPairs];
+#pragma unroll
+  for (int j = 0; j < NCH; ++j) {
+    float f[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) f[i] = 1.f;
+    if (p.w && (j * 32 + lane) * VEC < p.C) load_f32<VEC>(p.w + (j * 32 + lane) * VEC, f);
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+      dw[j][i] = db[j][i] = 0ull;
+      w[j][i] = pack2(f[2 * i], f[2 * i + 1]);
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) fetch(first + s * step, s);
+  const float inv_c = 1.f / (float)p.C;
+  int stage = 0;
+  for (int64_t row = first; row < p.rows; row += step) {
+    fetch(row + (kStages - 1) * step, stage == 0 ? kStages - 1 : stage - 1);
+    const float mean = __ldg(p.mean + row), rstd = __ldg(p.rstd + row);
+    const uint64_t nmean2 = pack2(-mean, -mean), rstd2 = pack2(rstd, rstd);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+    const unsigned char* at = mine + stage * 2 * NCH * 512;
+    auto pairs = [&](const unsigned char* src, uint64_t (&v)[kPairs]) {
+      Piece<T, VEC> q;
+      q.r = *reinterpret_cast<const decltype(q.r)*>(src);
+      float f[VEC];
+      q.get(f);
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) v[i] = pack2(f[2 * i], f[2 * i + 1]);
+    };
+    uint64_t s0 = 0ull, s1 = 0ull;
+#pragma unroll
+    for (int j = 0; j < NCH; ++j)
+      if ((j * 32 + lane) * VEC < p.C) {
+        uint64_t x[kPairs], d[kPairs];
+        pairs(at + j * 512, x);
+        pairs(at + (NCH + j) * 512, d);
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+          const uint64_t xh = mul2(add2(x[i], nmean2), rstd2), g = mul2(d[i], w[j][i]);
+          dw[j][i] = fma2(d[i], xh, dw[j][i]);
+          db[j][i] = add2(db[j][i], d[i]);
+          s0 = add2(s0, g);
+          s1 = fma2(g, xh, s1);
+        }
+      }
+    float a, b;
+    unpack2(s0, a, b);
+    const float mg = warp_sum(a + b) * inv_c;
+    unpack2(s1, a, b);
+    const float mgx = warp_sum(a + b) * inv_c;
+    const uint64_t nmg2 = pack2(-mg, -mg), nmgx2 = pack2(-mgx, -mgx);
+    T* dx = (T*)p.y + row * p.C;
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+      const int c = (j * 32 + lane) * VEC;
+      if (c < p.C) {
+        uint64_t x[kPairs], d[kPairs];
+        pairs(at + j * 512, x);
+        pairs(at + (NCH + j) * 512, d);
+        float f[VEC];
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+          const uint64_t xh = mul2(add2(x[i], nmean2), rstd2);
+          unpack2(mul2(rstd2, fma2(xh, nmgx2, fma2(d[i], w[j][i], nmg2))), f[2 * i], f[2 * i + 1]);
+        }
+        Piece<T, VEC> q;
+        q.set(f);
+        q.store(dx + c);
+      }
+    }
+    stage = stage + 1 == kStages ? 0 : stage + 1;
+  }
+  if (!p.partial) return;
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncwarp();                                           // (a warp's sums take its own ring's place)
+  constexpr int kCols = NCH * 32 * VEC;
+  float* own = reinterpret_cast<float*>(ring + (size_t)warp * kRing);
+#pragma unroll
+  for (int j = 0; j < NCH; ++j)
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+      const int c = (j * 32 + lane) * VEC + 2 * i;
+      *reinterpret_cast<uint64_t*>(own + c) = dw[j][i];
+      *reinterpret_cast<uint64_t*>(own + kCols + c) = db[j][i];
+    }
+  __syncthreads();
+  float* part = p.partial + (size_t)blockIdx.x * 2 * p.C;
+  for (int c = threadIdx.x; c < 2 * p.C; c += blockDim.x) {
+    const int at = c < p.C ? c : c - p.C + kCols;
+    float s = 0.f;
+    for (int k = 0; k < nwarps; ++k) s += reinterpret_cast<const float*>(ring + (size_t)k * kRing)[at];
+    part[c] = s;
   }
 }
 
+// ---- gradient of other rows: read value by value, or (BLOCK) longer than 1024 ----------------------------------------------
 // Shared memory: BLOCK: 128 floats; else the block's sums, 2 C floats, added to by its warps one after the other
 template <typename T, int VEC, int NCH, bool BLOCK>
 __global__ void __launch_bounds__(BLOCK ? 512 : 128, 1) layer_norm_grad_kernel(const NormParams p) {
@@ -305,21 +459,43 @@ bool norm_wide(const NormArgs& a) {
   return low % 16 == 0;
 }
 
+template <typename T, int VEC, int NCH>
+cudaError_t launch_norm_rows(const NormParams& p, int64_t blocks, cudaStream_t st) {
+  // Two rows of bf16 values a warp where there are enough to fill the chip all the same.  Measured, one / two / four rows a warp: 32768
+  // rows of 1024 values 27.3 / 24.1 / 24.4 us (5.6 TB/s, what a plain copy of this size reaches), of 384 13.8 / 12.9 / 12.9; fp32, whose rows
+  // are twice the bytes against the same weights, 21316 of 768: 22.5 / 22.7 / 23.1.
+  if (VEC == 8 && p.rows >= 2ll * 16 * device_sm_count())
+    return launch_programmatic(layer_norm_kernel<T, VEC, NCH, false, (VEC == 8 ? 2 : 1)>, dim3((unsigned)((blocks + 1) / 2)), kNormWarps * 32, 0, st, p);
+  return launch_programmatic(layer_norm_kernel<T, VEC, NCH, false, 1>, dim3((unsigned)blocks), kNormWarps * 32, 0, st, p);
+}
+template <typename T, int VEC, int NCH>
+cudaError_t launch_grad_rows(const NormParams& p, int64_t blocks, cudaStream_t st) {
+  if constexpr (VEC > 1) {
+    constexpr size_t smem = (size_t)kGradWarps * kGradStages<NCH> * 2 * NCH * 512;
+    static_assert(kGradStages<NCH> * 2 * NCH * 512 >= 2 * NCH * 32 * VEC * (int)sizeof(float), "a warp's sums take its ring's place");
+    static OncePerDevice opt_in;
+    const cudaError_t e = opt_in.run([] { return cudaFuncSetAttribute(layer_norm_grad_rows_kernel<T, VEC, NCH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
+    if (e != cudaSuccess) return e;
+    return launch_programmatic(layer_norm_grad_rows_kernel<T, VEC, NCH>, dim3((unsigned)blocks), kGradWarps * 32, smem, st, p);
+  } else {
+    return launch_programmatic(layer_norm_grad_kernel<T, VEC, NCH, false>, dim3((unsigned)blocks), kNormWarps * 32, 2 * (size_t)p.C * sizeof(float), st, p);
+  }
+}
+
 template <typename T, int VEC, bool GRAD>
 cudaError_t launch_norm(const NormArgs& a, const NormParams& p, int blocks, cudaStream_t st) {
   constexpr int kAll = 32 / VEC;        // pieces of a lane that holds 32 values
-  auto go = [&](auto kernel, bool block) -> cudaError_t {
-    const int warps = block ? norm_block_warps(a.C) : kNormWarps;
-    const size_t smem = !GRAD ? 0 : block ? 128 * sizeof(float) : 2 * (size_t)a.C * sizeof(float);
-    return launch_programmatic(kernel, dim3((unsigned)blocks), warps * 32, smem, st, p);
-  };
-  if (a.C > kWarpCols) return go(GRAD ? layer_norm_grad_kernel<T, VEC, kAll, true> : layer_norm_kernel<T, VEC, kAll, true>, true);
+  if (a.C > kWarpCols) {
+    const int threads = norm_block_warps(a.C) * 32;
+    if (GRAD) return launch_programmatic(layer_norm_grad_kernel<T, VEC, kAll, true>, dim3((unsigned)blocks), threads, 128 * sizeof(float), st, p);
+    return launch_programmatic(layer_norm_kernel<T, VEC, kAll, true, 1>, dim3((unsigned)blocks), threads, 0, st, p);
+  }
   const int quarter = (a.C + 255) / 256;                 // 8, 16, 24 or 32 values a lane
   switch (quarter) {
-    case 1: return go(GRAD ? layer_norm_grad_kernel<T, VEC, kAll / 4, false> : layer_norm_kernel<T, VEC, kAll / 4, false>, false);
-    case 2: return go(GRAD ? layer_norm_grad_kernel<T, VEC, kAll / 2, false> : layer_norm_kernel<T, VEC, kAll / 2, false>, false);
-    case 3: return go(GRAD ? layer_norm_grad_kernel<T, VEC, kAll / 4 * 3, false> : layer_norm_kernel<T, VEC, kAll / 4 * 3, false>, false);
-    default: return go(GRAD ? layer_norm_grad_kernel<T, VEC, kAll, false> : layer_norm_kernel<T, VEC, kAll, false>, false);
+    case 1: return GRAD ? launch_grad_rows<T, VEC, kAll / 4>(p, blocks, st) : launch_norm_rows<T, VEC, kAll / 4>(p, blocks, st);
+    case 2: return GRAD ? launch_grad_rows<T, VEC, kAll / 2>(p, blocks, st) : launch_norm_rows<T, VEC, kAll / 2>(p, blocks, st);
+    case 3: return GRAD ? launch_grad_rows<T, VEC, kAll / 4 * 3>(p, blocks, st) : launch_norm_rows<T, VEC, kAll / 4 * 3>(p, blocks, st);
+    default: return GRAD ? launch_grad_rows<T, VEC, kAll>(p, blocks, st) : launch_norm_rows<T, VEC, kAll>(p, blocks, st);
   }
 }
 
@@ -332,10 +508,18 @@ cudaError_t dispatch_norm(const NormArgs& a, const NormParams& p, int blocks, cu
 
 }  // namespace
 
-int layer_norm_grad_blocks(int64_t rows, int C) {
-  const int64_t per_block = C > kWarpCols ? 1 : kNormWarps;
-  const int64_t most = C > kWarpCols ? 2ll * device_sm_count() : 3ll * device_sm_count(), need = (rows + per_block - 1) / per_block;
+namespace {
+// Blocks of the gradient's launch: of twelve rows at a time, of four where rows are read value by value, of one where they are long
+int grad_blocks(int64_t rows, int C, bool wide) {
+  const int64_t per_block = C > kWarpCols ? 1 : wide ? kGradWarps : kNormWarps;
+  const int64_t most = (C > kWarpCols ? 2ll : wide ? 1ll : 3ll) * device_sm_count(), need = (rows + per_block - 1) / per_block;
   return (int)(need < most ? need : most);
+}
+}  // namespace
+
+int layer_norm_grad_blocks(int64_t rows, int C) {
+  const int a = grad_blocks(rows, C, false), b = grad_blocks(rows, C, true);
+  return a > b ? a : b;
 }
 
 cudaError_t launch_layer_norm(const NormArgs& a, cudaStream_t st) {
@@ -346,7 +530,7 @@ cudaError_t launch_layer_norm(const NormArgs& a, cudaStream_t st) {
 
 cudaError_t launch_layer_norm_grad(const NormArgs& a, float* partial, float* dw, float* db, cudaStream_t st) {
   const bool sums = dw || db;
-  const int blocks = layer_norm_grad_blocks(a.rows, a.C);
+  const int blocks = grad_blocks(a.rows, a.C, norm_wide(a));
   const NormParams p{a.x, a.dy, a.w, nullptr, a.y, a.mean, a.rstd, sums ? partial : nullptr, a.rows, a.x_stride, a.dy_stride, a.C, 0.f};
   const cudaError_t e = dispatch_norm<true>(a, p, blocks, st);
   if (e != cudaSuccess || !sums) return e;
