@@ -33,6 +33,7 @@ struct ScanArgs {
   Rows us, ds, bs, cs, zs;
 };
 struct ScanPlan {
+  int lanes;                         // of a channel
   int nchunk, chunk;                 // chunks of a sequence (1: no scratch) and their tokens
   size_t off_state, off_sum, total;  // bytes: [B, nchunk, C, Ns] states, [B, nchunk, C] sums of steps
 };

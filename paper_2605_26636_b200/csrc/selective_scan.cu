@@ -1,35 +1,50 @@
 // The selective scan of a state-space mixer: every channel carries Ns states through its sequence.
 //   d_t = softplus(dt_t + dt_bias),  h_t = exp(d_t A) h_(t-1) + d_t B_t u_t,  y_t = (C_t . h_t + D u_t) z_t / (1 + exp(-z_t))
 //
-// Four lanes share a channel, a quarter of its states each in registers; a warp has 8 channels, a block 64.  Tiles of 32 tokens of u, dt, z, B, C
-// pass through shared memory (the next one's loads are in flight meanwhile), where d_t and d_t u_t are formed once per token
-// and channel.  Four tokens at a time: the lanes' shares of four y are exchanged so that every lane ends up with the sum of one.
+// Four or eight lanes share a channel, each with a share of its states in registers; a block has 64 or 32 channels.  Tiles of 2048 values
+// (32 or 64 tokens) of u, dt, z pass through shared memory with their B and C (the next one's loads are in flight meanwhile), where
+// d_t and d_t u_t are formed once per token and channel.  As many tokens at a time as a channel has lanes: the lanes' shares
+// of their y are exchanged so that every lane ends up with the sum of one.  States in pairs (the packed fp32 arithmetic of sm_100).
 //
-// What bounds it: the exponentials, Ns a token and channel on the MUFU unit (16 a clock and SM), three times what
+// What bounds it: the exponentials, Ns a token and channel on the MUFU unit (16 a clock and SM), more than twice what
 // the bytes take at Ns = 16 in bf16.
 //
 // A sequence is cut into chunks where the channels alone leave SMs idle: one pass for the chunks' own states from zero, a
 // second that carries the state from chunk to chunk (h_end = exp(A sum d) h_begin + own), a third like the single pass, from
 // the states that the second left.
 #include "scan.cuh"
+#include "tc_common.cuh"   // packed fp32 arithmetic
 
 namespace jv {
 namespace {
 
-constexpr int kCh = 64;               // channels of a block
-constexpr int kLanes = 4;             // lanes of a channel
-constexpr int kThreads = kCh * kLanes;
-constexpr int kTT = 32;               // tokens of a tile
+using tc::add2;
+using tc::ex2;
+using tc::fma2;
+using tc::mul2;
+using tc::pack2;
+using tc::unpack2;
+
+constexpr int kThreads = 256;
+constexpr int kTile = 2048;           // tokens times channels of a tile
 constexpr int kStepTokens = 4;        // calls of at most this many tokens walk without tiles
 constexpr float kLog2e = 1.4426950408889634f;
 
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
+// log(1 + e^x) = max(x, 0) + log1p(t), t = e^-|x|;  log1p(t) = 2 artanh(t / (2 + t)), the series of artanh up to the 15th power:
+// its argument is 1/3 at most, so what is left out is below 2^-26 of it
+__device__ __forceinline__ float softplus(float x) {
+  const float t = ex2(-fabsf(x) * kLog2e), s = __fdividef(t, 2.f + t), q = s * s;
+  float a = fmaf(q, 1.f / 15.f, 1.f / 13.f);
+  a = fmaf(q, a, 1.f / 11.f);
+  a = fmaf(q, a, 1.f / 9.f);
+  a = fmaf(q, a, 1.f / 7.f);
+  a = fmaf(q, a, 1.f / 5.f);
+  a = fmaf(q, a, 1.f / 3.f);
+  a = fmaf(q, a, 1.f);
+  const float top = x > 0.f ? x : x == x ? 0.f : x;        // (no number stays none)
+  return fmaf(2.f * s, a, top);
 }
-__device__ __forceinline__ float softplus(float x) { return x > 20.f ? x : log1pf(__expf(x)); }
-__device__ __forceinline__ float silu(float x) { return x / (1.f + __expf(-x)); }
+__device__ __forceinline__ float silu(float x) { return __fdividef(x, 1.f + ex2(-x * kLog2e)); }
 
 __device__ __forceinline__ int length_of(const ScanArgs& a, int b) { return a.lens ? min(max(__ldg(a.lens + b), 0), a.L) : a.L; }
 
@@ -54,6 +69,7 @@ __device__ __forceinline__ void store_state(float* h, int Ns, int s, const float
 // ---- a few tokens: straight from global memory ------------------------------------------------------------------------
 template <typename T, int NPL>
 __global__ void __launch_bounds__(kThreads) scan_step_kernel(const ScanArgs a) {
+  constexpr int kLanes = 4, kCh = kThreads / kLanes;
   griddep_wait();
   griddep_launch_dependents();
   const int b = blockIdx.y, c = blockIdx.x * kCh + (int)threadIdx.x / kLanes, s = threadIdx.x % kLanes;
@@ -90,27 +106,30 @@ __global__ void __launch_bounds__(kThreads) scan_step_kernel(const ScanArgs a) {
 }
 
 // ---- tiles of tokens ------------------------------------------------------------------------------------------------------
-template <typename T, int NPL>
+template <typename T, int S, int NPL>
 struct Smem {
-  float d[kTT][kCh], du[kTT][kCh];
-  float Bm[kTT][kLanes * NPL], Cm[kTT][kLanes * NPL];
+  static constexpr int kCh = kThreads / S, kTT = kTile / kCh;
+  float4 d[kTT][kCh];                 // d, d, d u, d u: pairs as the arithmetic takes them
+  float bc[kTT][S][2 * NPL];          // B, then C, of a lane's states
   T u[kTT][kCh], z[kTT][kCh];         // u: y takes its place
 };
 
-// kY: the whole thing; else the chunk's own state from zero and the sum of its steps only
-template <typename T, int NPL, bool WIDE, bool kY>
-__global__ void __launch_bounds__(kThreads) scan_kernel(const ScanArgs a, int chunk, int nchunk, float* ws_state, float* ws_sum) {
+// S lanes a channel, NPL states a lane.  kY: the whole thing; else the chunk's own state from zero and the sum of its steps only
+template <typename T, int S, int NPL, bool WIDE, bool kY>
+__global__ void __launch_bounds__(kThreads, 2) scan_kernel(const ScanArgs a, int chunk, int nchunk, float* ws_state, float* ws_sum) {
+  using Sm = Smem<T, S, NPL>;
+  constexpr int kCh = Sm::kCh, kTT = Sm::kTT;
   constexpr int kVec = WIDE ? 16 / sizeof(T) : 1;             // elements of a load
-  constexpr int kLoads = kTT * kCh / kThreads / kVec;         // loads of a thread and tile from each of u, dt, z
+  constexpr int kLoads = kTile / kThreads / kVec;             // loads of a thread and tile from each of u, dt, z
   constexpr int kRow = kCh / kVec;                            // loads of a token
-  constexpr int kNs = kLanes * NPL;
+  constexpr int kNs = S * NPL;
   constexpr int kBC = (kTT * kNs + kThreads - 1) / kThreads;  // elements of a thread and tile from each of B, C
   extern __shared__ __align__(16) unsigned char smem_raw[];
-  Smem<T, NPL>& sm = *reinterpret_cast<Smem<T, NPL>*>(smem_raw);
+  Sm& sm = *reinterpret_cast<Sm*>(smem_raw);
   griddep_wait();
   griddep_launch_dependents();
   const int b = blockIdx.z, ck = blockIdx.y, c0 = blockIdx.x * kCh, tid = threadIdx.x;
-  const int lc = tid / kLanes, s = tid % kLanes, c = c0 + lc, cc = min(c, a.C - 1);
+  const int lc = tid / S, s = tid % S, c = c0 + lc, cc = min(c, a.C - 1);
   const int len = length_of(a, b);
   const int t_begin = ck * chunk, t_end = min(t_begin + chunk, len);
   const int64_t ch = ((int64_t)b * nchunk + ck) * a.C + cc;    // of the workspace's arrays
@@ -118,7 +137,23 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(const ScanArgs a, int ch
   load_A<NPL>(a, cc, s, A2);
   if (kY && nchunk > 1) load_state<NPL>(ws_state + ch * a.Ns, a.Ns, s, h);
   else load_state<NPL>(kY && a.h_in ? a.h_in + ((int64_t)b * a.C + cc) * a.Ns : nullptr, a.Ns, s, h);
+  constexpr int kPairs = NPL / 2;
+  uint64_t A2p[NPL > 1 ? kPairs : 1], hp[NPL > 1 ? kPairs : 1];
+#pragma unroll
+  for (int n = 0; n < kPairs; ++n) {
+    A2p[n] = pack2(A2[2 * n], A2[2 * n + 1]);
+    hp[n] = pack2(h[2 * n], h[2 * n + 1]);
+  }
   const float D = a.D ? __ldg(a.D + cc) : 0.f;
+  float bias[kVec];                                             // of the columns that this thread loads
+#pragma unroll
+  for (int v = 0; v < kVec; ++v) bias[v] = 0.f;
+  constexpr bool kOneColumn = kThreads % kRow == 0;             // every load of a thread is of the same columns
+  static_assert(kOneColumn, "a thread's loads are of one set of columns");
+  const int lcol = (tid % kRow) * kVec;
+  if (a.dt_bias)
+#pragma unroll
+    for (int v = 0; v < kVec; ++v) bias[v] = __ldg(a.dt_bias + min(c0 + lcol + v, a.C - 1));
 
   using Raw = typename std::conditional<WIDE, uint4, T>::type;
   Raw ru[kLoads], rd[kLoads], rz[kLoads];
@@ -126,7 +161,7 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(const ScanArgs a, int ch
   auto fetch = [&](int t0) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int e = i * kThreads + tid, t = t0 + e / kRow, col = c0 + (e % kRow) * kVec;
+      const int t = t0 + (i * kThreads + tid) / kRow, col = c0 + lcol;
       const bool in = t < t_end && col < a.C;                  // (16 bytes at a time: C is a multiple of them)
       Raw zero;
       memset(&zero, 0, sizeof(Raw));
@@ -145,40 +180,39 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(const ScanArgs a, int ch
   auto put = [&](int t0) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int e = i * kThreads + tid, t = e / kRow, col = (e % kRow) * kVec;
+      const int t = (i * kThreads + tid) / kRow;
       T uu[kVec], dd[kVec];
       memcpy(uu, &ru[i], sizeof(Raw));
       memcpy(dd, &rd[i], sizeof(Raw));
 #pragma unroll
       for (int v = 0; v < kVec; ++v) {
-        float d = 0.f;                                          // a token past the end: exp(0) h + 0
-        if (t0 + t < t_end) {
-          d = to_f32(dd[v]) + (a.dt_bias ? __ldg(a.dt_bias + min(c0 + col + v, a.C - 1)) : 0.f);
-          if (a.softplus) d = softplus(d);
-        }
-        sm.d[t][col + v] = d;
-        sm.du[t][col + v] = d * to_f32(uu[v]);
+        float d = to_f32(dd[v]) + bias[v];
+        if (a.softplus) d = softplus(d);
+        if (t0 + t >= t_end) d = 0.f;                           // a token past the end: exp(0) h + 0
+        const float du = d * to_f32(uu[v]);
+        sm.d[t][lcol + v] = make_float4(d, d, du, du);
       }
       if (kY) {
-        *reinterpret_cast<Raw*>(&sm.u[t][col]) = ru[i];
-        *reinterpret_cast<Raw*>(&sm.z[t][col]) = rz[i];
+        *reinterpret_cast<Raw*>(&sm.u[t][lcol]) = ru[i];
+        *reinterpret_cast<Raw*>(&sm.z[t][lcol]) = rz[i];
       }
     }
 #pragma unroll
     for (int i = 0; i < kBC; ++i) {
       const int e = i * kThreads + tid;
       if (e < kTT * kNs) {
-        sm.Bm[e / kNs][e % kNs] = to_f32(rb[i]);
-        if (kY) sm.Cm[e / kNs][e % kNs] = to_f32(rc[i]);
+        const int n = e % kNs;
+        sm.bc[e / kNs][n / NPL][n % NPL] = to_f32(rb[i]);
+        if (kY) sm.bc[e / kNs][n / NPL][NPL + n % NPL] = to_f32(rc[i]);
       }
     }
   };
   auto flush = [&](int t0) {                                    // the tile of y to global memory
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int e = i * kThreads + tid, t = e / kRow, col = (e % kRow) * kVec;
-      if (t0 + t < t_end && c0 + col < a.C)
-        *reinterpret_cast<Raw*>((T*)a.y + ((int64_t)b * a.L + t0 + t) * a.C + c0 + col) = *reinterpret_cast<const Raw*>(&sm.u[t][col]);
+      const int t = (i * kThreads + tid) / kRow;
+      if (t0 + t < t_end && c0 + lcol < a.C)
+        *reinterpret_cast<Raw*>((T*)a.y + ((int64_t)b * a.L + t0 + t) * a.C + c0 + lcol) = *reinterpret_cast<const Raw*>(&sm.u[t][lcol]);
     }
   };
 
@@ -187,27 +221,60 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(const ScanArgs a, int ch
     put(t0);
     __syncthreads();
     if (t0 + kTT < t_end) fetch(t0 + kTT);
-#pragma unroll 2
-    for (int t = 0; t < kTT; t += kLanes) {
-      float y[kLanes];
+    const int tokens = min(kTT, t_end - t0);
+#pragma unroll 1
+    for (int t = 0; t < tokens; t += S) {                       // (kTT is a multiple of S; tokens past the end change nothing)
+      float y[S];
 #pragma unroll
-      for (int j = 0; j < kLanes; ++j) {
-        const float d = sm.d[t + j][lc], du = sm.du[t + j][lc];
-        y[j] = 0.f;
-        if (!kY) sum += d;
+      for (int j = 0; j < S; ++j) {
+        const float4 q = sm.d[t + j][lc];
+        const float* bc = sm.bc[t + j][s];
+        if (!kY) sum += q.x;
+        if constexpr (NPL == 1) {
+          h[0] = fmaf(ex2(q.x * A2[0]), h[0], q.z * bc[0]);
+          if (kY) y[j] = h[0] * bc[1];
+        } else {
+          constexpr int kUse = kY ? 2 * NPL : NPL;              // B, and C
+          float v[kUse];
 #pragma unroll
-        for (int n = 0; n < NPL; ++n) {
-          h[n] = fmaf(ex2(d * A2[n]), h[n], du * sm.Bm[t + j][s * NPL + n]);
-          if (kY) y[j] = fmaf(h[n], sm.Cm[t + j][s * NPL + n], y[j]);
+          for (int n = 0; n < kUse; n += kUse % 4 ? 2 : 4) {
+            if constexpr (kUse % 4) {
+              const float2 x = *reinterpret_cast<const float2*>(bc + n);
+              v[n] = x.x; v[n + 1] = x.y;
+            } else {
+              const float4 x = *reinterpret_cast<const float4*>(bc + n);
+              v[n] = x.x; v[n + 1] = x.y; v[n + 2] = x.z; v[n + 3] = x.w;
+            }
+          }
+          const uint64_t dd = pack2(q.x, q.y), du = pack2(q.z, q.w);
+          uint64_t yp = 0ull;
+#pragma unroll
+          for (int n = 0; n < kPairs; ++n) {
+            float e0, e1;
+            unpack2(mul2(dd, A2p[n]), e0, e1);
+            hp[n] = fma2(pack2(ex2(e0), ex2(e1)), hp[n], mul2(du, pack2(v[2 * n], v[2 * n + 1])));
+            if constexpr (kY) {
+              const uint64_t cn = pack2(v[NPL + 2 * n], v[NPL + 2 * n + 1]);
+              yp = n == 0 ? mul2(hp[n], cn) : fma2(hp[n], cn, yp);
+            }
+          }
+          if (kY) {
+            float y0, y1;
+            unpack2(yp, y0, y1);
+            y[j] = y0 + y1;
+          }
         }
       }
       if (kY) {
-        // lanes s and s ^ 1 exchange: an even one keeps tokens 0 and 2, an odd one 1 and 3; then s and s ^ 2
-        const float a0 = (s & 1) ? y[1] : y[0], a1 = (s & 1) ? y[3] : y[2], o0 = (s & 1) ? y[0] : y[1], o1 = (s & 1) ? y[2] : y[3];
-        const float p0 = a0 + __shfl_xor_sync(0xffffffffu, o0, 1), p1 = a1 + __shfl_xor_sync(0xffffffffu, o1, 1);
-        float r = (s & 2) ? p1 : p0;
-        r += __shfl_xor_sync(0xffffffffu, (s & 2) ? p0 : p1, 2);   // token t + s
-        r = fmaf(D, to_f32(sm.u[t + s][lc]), r);
+        // lanes that differ in bit k of their number exchange: each keeps the tokens whose bit k is its own, and token t + s is left
+#pragma unroll
+        for (int k = 1, left = S; left > 1; k <<= 1, left >>= 1)
+#pragma unroll
+          for (int i = 0; i < left / 2; ++i) {
+            const float give = (s & k) ? y[2 * i] : y[2 * i + 1], keep = (s & k) ? y[2 * i + 1] : y[2 * i];
+            y[i] = keep + __shfl_xor_sync(0xffffffffu, give, k);
+          }
+        float r = fmaf(D, to_f32(sm.u[t + s][lc]), y[0]);
         if (a.z) r *= silu(to_f32(sm.z[t + s][lc]));
         from_f32(&sm.u[t + s][lc], r);
       }
@@ -216,6 +283,8 @@ __global__ void __launch_bounds__(kThreads) scan_kernel(const ScanArgs a, int ch
     if (kY) flush(t0);                                          // (a thread reads and refills the same places of u)
   }
   if (c >= a.C) return;
+#pragma unroll
+  for (int n = 0; n < kPairs; ++n) unpack2(hp[n], h[2 * n], h[2 * n + 1]);
   if (kY) {
     // the state behind the last token: by the chunk that has it, the first one of an empty sequence
     if (a.h_out && (t_begin < t_end ? t_end == len : len == 0 && ck == 0)) store_state<NPL>(a.h_out + ((int64_t)b * a.C + c) * a.Ns, a.Ns, s, h);
@@ -244,57 +313,74 @@ __global__ void __launch_bounds__(256) scan_carry_kernel(const ScanArgs a, int n
   }
 }
 
-template <typename T, int NPL, bool WIDE>
+template <typename T, int S, int NPL, bool WIDE>
 cudaError_t launch_tiles(const ScanArgs& a, const ScanPlan& p, void* ws, cudaStream_t st) {
-  const dim3 grid((unsigned)ceil_div(a.C, kCh), (unsigned)p.nchunk, (unsigned)a.B);
-  const size_t smem = sizeof(Smem<T, NPL>);
+  using Sm = Smem<T, S, NPL>;
+  const dim3 grid((unsigned)ceil_div(a.C, Sm::kCh), (unsigned)p.nchunk, (unsigned)a.B);
   static OncePerDevice opt_in;
   cudaError_t e = opt_in.run([] {
-    const cudaError_t r = cudaFuncSetAttribute(scan_kernel<T, NPL, WIDE, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<T, NPL>));
-    return r != cudaSuccess ? r : cudaFuncSetAttribute(scan_kernel<T, NPL, WIDE, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<T, NPL>));
+    const cudaError_t r = cudaFuncSetAttribute(scan_kernel<T, S, NPL, WIDE, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Sm));
+    return r != cudaSuccess ? r : cudaFuncSetAttribute(scan_kernel<T, S, NPL, WIDE, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Sm));
   });
   if (e != cudaSuccess) return e;
   float* state = p.nchunk > 1 ? (float*)((char*)ws + p.off_state) : nullptr;
   float* sum = p.nchunk > 1 ? (float*)((char*)ws + p.off_sum) : nullptr;
   if (p.nchunk > 1) {
-    e = launch_programmatic(scan_kernel<T, NPL, WIDE, false>, grid, kThreads, smem, st, a, p.chunk, p.nchunk, state, sum);
+    e = launch_programmatic(scan_kernel<T, S, NPL, WIDE, false>, grid, kThreads, sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
     if (e != cudaSuccess) return e;
     const int64_t n = (int64_t)a.B * a.C * a.Ns;
     e = launch_programmatic(scan_carry_kernel, dim3((unsigned)((n + 255) / 256)), 256, 0, st, a, p.nchunk, state, (const float*)sum);
     if (e != cudaSuccess) return e;
   }
-  return launch_programmatic(scan_kernel<T, NPL, WIDE, true>, grid, kThreads, smem, st, a, p.chunk, p.nchunk, state, sum);
+  return launch_programmatic(scan_kernel<T, S, NPL, WIDE, true>, grid, kThreads, sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
 }
 
-template <typename T, int NPL>
+template <typename T, int S, int NPL>
 cudaError_t launch_states(const ScanArgs& a, const ScanPlan& p, void* ws, cudaStream_t st) {
-  if (a.L <= kStepTokens) return launch_programmatic(scan_step_kernel<T, NPL>, dim3((unsigned)ceil_div(a.C, kCh), (unsigned)a.B), kThreads, 0, st, a);
   const size_t e = sizeof(T);
   const bool wide = ((uintptr_t)a.u | (uintptr_t)a.dt | (uintptr_t)a.z | (uintptr_t)a.y | a.C * e | a.us.tok * e | a.us.batch * e |
                      a.ds.tok * e | a.ds.batch * e | (a.z ? (a.zs.tok | a.zs.batch) * e : 0)) % 16 == 0;
-  return wide ? launch_tiles<T, NPL, true>(a, p, ws, st) : launch_tiles<T, NPL, false>(a, p, ws, st);
+  return wide ? launch_tiles<T, S, NPL, true>(a, p, ws, st) : launch_tiles<T, S, NPL, false>(a, p, ws, st);
 }
 
 template <typename T>
 cudaError_t launch_type(const ScanArgs& a, const ScanPlan& p, void* ws, cudaStream_t st) {
-  const int npl = ceil_div(a.Ns, kLanes);
-  if (npl <= 1) return launch_states<T, 1>(a, p, ws, st);
-  if (npl <= 2) return launch_states<T, 2>(a, p, ws, st);
-  if (npl <= 4) return launch_states<T, 4>(a, p, ws, st);
-  if (npl <= 8) return launch_states<T, 8>(a, p, ws, st);
-  return launch_states<T, 16>(a, p, ws, st);
+  if (a.L <= kStepTokens) {
+    const dim3 grid((unsigned)ceil_div(a.C, kThreads / 4), (unsigned)a.B);
+    const int npl = ceil_div(a.Ns, 4);
+    if (npl <= 1) return launch_programmatic(scan_step_kernel<T, 1>, grid, kThreads, 0, st, a);
+    if (npl <= 2) return launch_programmatic(scan_step_kernel<T, 2>, grid, kThreads, 0, st, a);
+    if (npl <= 4) return launch_programmatic(scan_step_kernel<T, 4>, grid, kThreads, 0, st, a);
+    if (npl <= 8) return launch_programmatic(scan_step_kernel<T, 8>, grid, kThreads, 0, st, a);
+    return launch_programmatic(scan_step_kernel<T, 16>, grid, kThreads, 0, st, a);
+  }
+  const int npl = ceil_div(a.Ns, p.lanes);
+  if (p.lanes == 4) {
+    if (npl <= 1) return launch_states<T, 4, 1>(a, p, ws, st);
+    if (npl <= 2) return launch_states<T, 4, 2>(a, p, ws, st);
+    if (npl <= 4) return launch_states<T, 4, 4>(a, p, ws, st);
+    return launch_states<T, 4, 8>(a, p, ws, st);
+  }
+  if (npl <= 1) return launch_states<T, 8, 1>(a, p, ws, st);
+  if (npl <= 2) return launch_states<T, 8, 2>(a, p, ws, st);
+  if (npl <= 4) return launch_states<T, 8, 4>(a, p, ws, st);
+  return launch_states<T, 8, 8>(a, p, ws, st);
 }
 
 }  // namespace
 
 ScanPlan scan_plan(int B, int L, int C, int Ns) {
-  ScanPlan p{1, L, 0, 0, 0};
+  ScanPlan p{4, 1, L, 0, 0, 0};
   if (L <= kStepTokens) return p;
-  // one pass where the channels give every SM a block; else chunks (which walk the exponentials twice) for two blocks an SM
-  const int64_t blocks = (int64_t)B * ceil_div(C, kCh), sms = device_sm_count();
+  // Four lanes a channel where the channels give every SM two blocks all the same, else eight (and above 32 states, which eight
+  // lanes hold); chunks, which walk the exponentials twice, where even those leave half the SMs idle
+  const int64_t sms = device_sm_count();
+  p.lanes = Ns > 32 || (int64_t)B * ceil_div(C, kThreads / 4) < 2 * sms ? 8 : 4;
+  const int64_t blocks = (int64_t)B * ceil_div(C, kThreads / p.lanes);
+  const int tt = kTile / (kThreads / p.lanes);
   if (blocks < sms / 2) {
-    const int want = (int)(2 * sms / blocks), tiles = ceil_div(L, kTT);
-    p.chunk = ceil_div(tiles, want < tiles ? want : tiles) * kTT;
+    const int want = (int)(2 * sms / blocks), tiles = ceil_div(L, tt);
+    p.chunk = ceil_div(tiles, want < tiles ? want : tiles) * tt;
     p.nchunk = ceil_div(L, p.chunk);
   }
   if (p.nchunk > 1) {
