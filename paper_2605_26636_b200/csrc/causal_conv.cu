@@ -78,12 +78,27 @@ __global__ void __launch_bounds__(kThreads) causal_conv_kernel(const ConvArgs a,
 #pragma unroll
     for (int i = 0; i < VEC; ++i) past[j][i] = old[j][i];
   }
-  float w[VEC][K], bias[VEC];
+  float w[VEC][K], bias[VEC];                      // (a thread's filters are VEC * K consecutive values: 16 bytes at a time)
+  if constexpr (VEC > 1) {
+    float f[VEC * K];
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) {
+    for (int i = 0; i < VEC * K; i += 4) {
+      const float4 v = __ldg(reinterpret_cast<const float4*>(a.w + (int64_t)c * K + i));
+      f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w;
+    }
 #pragma unroll
-    for (int j = 0; j < K; ++j) w[i][j] = __ldg(a.w + (int64_t)(c + i) * K + j);
-    bias[i] = a.b ? __ldg(a.b + c + i) : 0.f;
+    for (int i = 0; i < VEC; ++i)
+#pragma unroll
+      for (int j = 0; j < K; ++j) w[i][j] = f[i * K + j];
+#pragma unroll
+    for (int i = 0; i < VEC; i += 4) {
+      const float4 v = a.b ? __ldg(reinterpret_cast<const float4*>(a.b + c + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      bias[i] = v.x; bias[i + 1] = v.y; bias[i + 2] = v.z; bias[i + 3] = v.w;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < K; ++j) w[0][j] = __ldg(a.w + (int64_t)c * K + j);
+    bias[0] = a.b ? __ldg(a.b + c) : 0.f;
   }
   for (int t = t0; t < t1; t += kAhead) {
     float in[kAhead][VEC];
@@ -100,7 +115,7 @@ __global__ void __launch_bounds__(kThreads) causal_conv_kernel(const ConvArgs a,
 #pragma unroll
           for (int j = 0; j < K - 1; ++j) s = fmaf(w[i][j], past[j][i], s);
           s = fmaf(w[i][K - 1], in[n][i], s);
-          o[i] = a.silu ? s / (1.f + __expf(-s)) : s;
+          o[i] = a.silu ? __fdividef(s, 1.f + __expf(-s)) : s;
 #pragma unroll
           for (int j = 0; j + 1 < K - 1; ++j) past[j][i] = past[j + 1][i];
           past[K - 2][i] = in[n][i];
@@ -144,7 +159,7 @@ cudaError_t launch(const ConvArgs& a, cudaStream_t st) {
 
 cudaError_t launch_causal_conv(const ConvArgs& a, cudaStream_t st) {
   const size_t e = a.dtype == JV_F32 ? 4 : 2;
-  const bool wide = ((uintptr_t)a.x | (uintptr_t)a.u | (uintptr_t)a.s_in | (uintptr_t)a.s_out | a.C * e | a.xs.tok * e | a.xs.batch * e) % 16 == 0;
+  const bool wide = ((uintptr_t)a.x | (uintptr_t)a.u | (uintptr_t)a.s_in | (uintptr_t)a.s_out | (uintptr_t)a.w | (uintptr_t)a.b | a.C * e | a.xs.tok * e | a.xs.batch * e) % 16 == 0;
   if (a.dtype == JV_F32) return wide ? launch<float, 4>(a, st) : launch<float, 1>(a, st);
   return wide ? launch<__nv_bfloat16, 8>(a, st) : launch<__nv_bfloat16, 1>(a, st);
 }

@@ -1,9 +1,10 @@
 // The selective scan of a state-space mixer: every channel carries Ns states through its sequence.
 //   d_t = softplus(dt_t + dt_bias),  h_t = exp(d_t A) h_(t-1) + d_t B_t u_t,  y_t = (C_t . h_t + D u_t) z_t / (1 + exp(-z_t))
 //
-// Four or eight lanes share a channel, each with a share of its states in registers; a block has 64 or 32 channels.  Tiles of 2048 values
-// (32 or 64 tokens) of u, dt, z pass through shared memory with their B and C (the next one's loads are in flight meanwhile), where
-// d_t and d_t u_t are formed once per token and channel.  As many tokens at a time as a channel has lanes: the lanes' shares
+// Four or eight lanes share a channel, each with a share of its states in registers; a block has 64 or 32 channels in eight warps.  Four
+// more warps bring tiles of 2048 values (32 or 64 tokens) of u, dt, z with their B and C into one of two buffers in shared memory,
+// form d_t and d_t u_t once per token and channel on the way, and take y out of them.  (Bringing tiles in between steps of the eight
+// warps themselves left both kinds of work waiting: two prompts of 4096 tokens, 2048 channels, 16 states 231 us.)  As many tokens at a time as a channel has lanes: the lanes' shares
 // of their y are exchanged so that every lane ends up with the sum of one.  States in pairs (the packed fp32 arithmetic of sm_100).
 //
 // What bounds it: the exponentials, Ns a token and channel on the MUFU unit (16 a clock and SM), more than twice what
@@ -25,7 +26,8 @@ using tc::mul2;
 using tc::pack2;
 using tc::unpack2;
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;         // that compute
+constexpr int kStagers = 128;         // that bring tiles in and out
 constexpr int kTile = 2048;           // tokens times channels of a tile
 constexpr int kStepTokens = 4;        // calls of at most this many tokens walk without tiles
 constexpr float kLog2e = 1.4426950408889634f;
@@ -109,29 +111,149 @@ __global__ void __launch_bounds__(kThreads) scan_step_kernel(const ScanArgs a) {
 template <typename T, int S, int NPL>
 struct Smem {
   static constexpr int kCh = kThreads / S, kTT = kTile / kCh;
-  float4 d[kTT][kCh];                 // d, d, d u, d u: pairs as the arithmetic takes them
-  float bc[kTT][S][2 * NPL];          // B, then C, of a lane's states
+  // bf16 pairs of B and C stay as they are: what a lane's registers take from shared memory, 32 lanes x 4 bytes a clock, is the
+  // tightest resource beside the exponentials
+  static constexpr bool kPacked = sizeof(T) == 2 && NPL > 1;
+  using Pack = typename std::conditional<kPacked, T, float>::type;
+  float2 d[kTT][kCh];                 // d, d u
+  Pack bc[kTT][S][2 * NPL];           // B, then C, of a lane's states
   T u[kTT][kCh], z[kTT][kCh];         // u: y takes its place
 };
 
-// S lanes a channel, NPL states a lane.  kY: the whole thing; else the chunk's own state from zero and the sum of its steps only
+// Barriers of a block: a buffer is full (all of it waits for the four warps); a buffer is done with (the four warps wait for the others)
+constexpr int kFull = 1, kDone = 3;
+__device__ __forceinline__ void barrier_sync(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kThreads + kStagers) : "memory"); }
+__device__ __forceinline__ void barrier_arrive(int id) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(kThreads + kStagers) : "memory"); }
+
+// The four warps that bring tiles in, two ahead of the others, and y out
 template <typename T, int S, int NPL, bool WIDE, bool kY>
-__global__ void __launch_bounds__(kThreads, 2) scan_kernel(const ScanArgs a, int chunk, int nchunk, float* ws_state, float* ws_sum) {
+__device__ __forceinline__ void stage_tiles(const ScanArgs& a, Smem<T, S, NPL>* buf, int b, int c0, int t_begin, int t_end, int tiles) {
   using Sm = Smem<T, S, NPL>;
   constexpr int kCh = Sm::kCh, kTT = Sm::kTT;
   constexpr int kVec = WIDE ? 16 / sizeof(T) : 1;             // elements of a load
-  constexpr int kLoads = kTile / kThreads / kVec;             // loads of a thread and tile from each of u, dt, z
+  constexpr int kLoads = kTile / kStagers / kVec;             // loads of a thread and tile from each of u, dt, z
   constexpr int kRow = kCh / kVec;                            // loads of a token
   constexpr int kNs = S * NPL;
-  constexpr int kBC = (kTT * kNs + kThreads - 1) / kThreads;  // elements of a thread and tile from each of B, C
+  constexpr int kBC = (kTT * kNs + kStagers - 1) / kStagers;  // elements of a thread and tile from each of B, C
+  const int tid = threadIdx.x - kThreads;
+  float bias[kVec];                                             // of the columns that this thread loads
+#pragma unroll
+  for (int v = 0; v < kVec; ++v) bias[v] = 0.f;
+  constexpr bool kOneColumn = kStagers % kRow == 0;             // every load of a thread is of the same columns
+  static_assert(kOneColumn, "a thread's loads are of one set of columns");
+  const int lcol = (tid % kRow) * kVec;
+  if (a.dt_bias)
+#pragma unroll
+    for (int v = 0; v < kVec; ++v) bias[v] = __ldg(a.dt_bias + min(c0 + lcol + v, a.C - 1));
+
+  using Raw = typename std::conditional<WIDE, uint4, T>::type;
+  Raw ru[kLoads], rd[kLoads], rz[kLoads];
+  T rb[kBC], rc[kBC];
+  auto fetch = [&](int t0) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int t = t0 + (i * kStagers + tid) / kRow, col = c0 + lcol;
+      const bool in = t < t_end && col < a.C;                  // (16 bytes at a time: C is a multiple of them)
+      Raw zero;
+      memset(&zero, 0, sizeof(Raw));
+      ru[i] = in ? *reinterpret_cast<const Raw*>((const T*)a.u + a.us.at(b, t) + col) : zero;
+      rd[i] = in ? *reinterpret_cast<const Raw*>((const T*)a.dt + a.ds.at(b, t) + col) : zero;
+      if (kY) rz[i] = in && a.z ? *reinterpret_cast<const Raw*>((const T*)a.z + a.zs.at(b, t) + col) : zero;
+    }
+#pragma unroll
+    for (int i = 0; i < kBC; ++i) {
+      const int e = i * kStagers + tid, t = t0 + e / kNs, n = e % kNs;
+      const bool in = t < t_end && n < a.Ns && e < kTT * kNs;
+      rb[i] = in ? ((const T*)a.Bm)[a.bs.at(b, t) + n] : T(0.f);
+      if (kY) rc[i] = in ? ((const T*)a.Cm)[a.cs.at(b, t) + n] : T(0.f);
+    }
+  };
+  auto put = [&](Sm& sm, int t0) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int t = (i * kStagers + tid) / kRow;
+      T uu[kVec], dd[kVec];
+      memcpy(uu, &ru[i], sizeof(Raw));
+      memcpy(dd, &rd[i], sizeof(Raw));
+      float d_even = 0.f, du_even = 0.f;
+#pragma unroll
+      for (int v = 0; v < kVec; ++v) {
+        float d = to_f32(dd[v]) + bias[v];
+        if (a.softplus) d = softplus(d);
+        if (t0 + t >= t_end) d = 0.f;                           // a token past the end: exp(0) h + 0
+        const float du = d * to_f32(uu[v]);
+        if constexpr (kVec == 1) {
+          sm.d[t][lcol] = make_float2(d, du);
+        } else {
+          if (v & 1) *reinterpret_cast<float4*>(&sm.d[t][lcol + v - 1]) = make_float4(d_even, du_even, d, du);
+          d_even = d;
+          du_even = du;
+        }
+      }
+      if (kY) {
+        *reinterpret_cast<Raw*>(&sm.u[t][lcol]) = ru[i];
+        *reinterpret_cast<Raw*>(&sm.z[t][lcol]) = rz[i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kBC; ++i) {
+      const int e = i * kStagers + tid;
+      if (e < kTT * kNs) {
+        const int n = e % kNs;
+        if constexpr (Sm::kPacked) {
+          sm.bc[e / kNs][n / NPL][n % NPL] = rb[i];
+          if (kY) sm.bc[e / kNs][n / NPL][NPL + n % NPL] = rc[i];
+        } else {
+          sm.bc[e / kNs][n / NPL][n % NPL] = to_f32(rb[i]);
+          if (kY) sm.bc[e / kNs][n / NPL][NPL + n % NPL] = to_f32(rc[i]);
+        }
+      }
+    }
+  };
+  auto flush = [&](const Sm& sm, int t0) {                                    // the tile of y to global memory
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int t = (i * kStagers + tid) / kRow;
+      if (t0 + t < t_end && c0 + lcol < a.C)
+        *reinterpret_cast<Raw*>((T*)a.y + ((int64_t)b * a.L + t0 + t) * a.C + c0 + lcol) = *reinterpret_cast<const Raw*>(&sm.u[t][lcol]);
+    }
+  };
+
+  for (int i = 0; i < min(2, tiles); ++i) {
+    fetch(t_begin + i * kTT);
+    put(buf[i], t_begin + i * kTT);
+    barrier_arrive(kFull + i);
+  }
+  for (int i = 0; i < tiles; ++i) {
+    const int t0 = t_begin + i * kTT;
+    if (i + 2 < tiles) fetch(t0 + 2 * kTT);
+    barrier_sync(kDone + (i & 1));
+    if (kY) flush(buf[i & 1], t0);                              // (a thread reads and refills the same places of u)
+    if (i + 2 < tiles) {
+      put(buf[i & 1], t0 + 2 * kTT);
+      barrier_arrive(kFull + (i & 1));
+    }
+  }
+}
+
+// S lanes a channel, NPL states a lane.  kY: the whole thing; else the chunk's own state from zero and the sum of its steps only
+template <typename T, int S, int NPL, bool WIDE, bool kY>
+__global__ void __launch_bounds__(kThreads + kStagers, 1) scan_kernel(const ScanArgs a, int chunk, int nchunk, float* ws_state, float* ws_sum) {
+  using Sm = Smem<T, S, NPL>;
+  constexpr int kCh = Sm::kCh, kTT = Sm::kTT;
   extern __shared__ __align__(16) unsigned char smem_raw[];
-  Sm& sm = *reinterpret_cast<Sm*>(smem_raw);
+  Sm* buf = reinterpret_cast<Sm*>(smem_raw);
   griddep_wait();
   griddep_launch_dependents();
   const int b = blockIdx.z, ck = blockIdx.y, c0 = blockIdx.x * kCh, tid = threadIdx.x;
-  const int lc = tid / S, s = tid % S, c = c0 + lc, cc = min(c, a.C - 1);
   const int len = length_of(a, b);
-  const int t_begin = ck * chunk, t_end = min(t_begin + chunk, len);
+  const int t_begin = ck * chunk, t_end = min(t_begin + chunk, len), tiles = max(0, (t_end - t_begin + kTT - 1) / kTT);
+
+  if (tid >= kThreads) {
+    stage_tiles<T, S, NPL, WIDE, kY>(a, buf, b, c0, t_begin, t_end, tiles);
+    return;
+  }
+  const int lc = tid / S, s = tid % S, c = c0 + lc, cc = min(c, a.C - 1);
   const int64_t ch = ((int64_t)b * nchunk + ck) * a.C + cc;    // of the workspace's arrays
   float A2[NPL], h[NPL], sum = 0.f;
   load_A<NPL>(a, cc, s, A2);
@@ -145,108 +267,46 @@ __global__ void __launch_bounds__(kThreads, 2) scan_kernel(const ScanArgs a, int
     hp[n] = pack2(h[2 * n], h[2 * n + 1]);
   }
   const float D = a.D ? __ldg(a.D + cc) : 0.f;
-  float bias[kVec];                                             // of the columns that this thread loads
-#pragma unroll
-  for (int v = 0; v < kVec; ++v) bias[v] = 0.f;
-  constexpr bool kOneColumn = kThreads % kRow == 0;             // every load of a thread is of the same columns
-  static_assert(kOneColumn, "a thread's loads are of one set of columns");
-  const int lcol = (tid % kRow) * kVec;
-  if (a.dt_bias)
-#pragma unroll
-    for (int v = 0; v < kVec; ++v) bias[v] = __ldg(a.dt_bias + min(c0 + lcol + v, a.C - 1));
-
-  using Raw = typename std::conditional<WIDE, uint4, T>::type;
-  Raw ru[kLoads], rd[kLoads], rz[kLoads];
-  T rb[kBC], rc[kBC];
-  auto fetch = [&](int t0) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int t = t0 + (i * kThreads + tid) / kRow, col = c0 + lcol;
-      const bool in = t < t_end && col < a.C;                  // (16 bytes at a time: C is a multiple of them)
-      Raw zero;
-      memset(&zero, 0, sizeof(Raw));
-      ru[i] = in ? *reinterpret_cast<const Raw*>((const T*)a.u + a.us.at(b, t) + col) : zero;
-      rd[i] = in ? *reinterpret_cast<const Raw*>((const T*)a.dt + a.ds.at(b, t) + col) : zero;
-      if (kY) rz[i] = in && a.z ? *reinterpret_cast<const Raw*>((const T*)a.z + a.zs.at(b, t) + col) : zero;
-    }
-#pragma unroll
-    for (int i = 0; i < kBC; ++i) {
-      const int e = i * kThreads + tid, t = t0 + e / kNs, n = e % kNs;
-      const bool in = t < t_end && n < a.Ns && e < kTT * kNs;
-      rb[i] = in ? ((const T*)a.Bm)[a.bs.at(b, t) + n] : T(0.f);
-      if (kY) rc[i] = in ? ((const T*)a.Cm)[a.cs.at(b, t) + n] : T(0.f);
-    }
-  };
-  auto put = [&](int t0) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int t = (i * kThreads + tid) / kRow;
-      T uu[kVec], dd[kVec];
-      memcpy(uu, &ru[i], sizeof(Raw));
-      memcpy(dd, &rd[i], sizeof(Raw));
-#pragma unroll
-      for (int v = 0; v < kVec; ++v) {
-        float d = to_f32(dd[v]) + bias[v];
-        if (a.softplus) d = softplus(d);
-        if (t0 + t >= t_end) d = 0.f;                           // a token past the end: exp(0) h + 0
-        const float du = d * to_f32(uu[v]);
-        sm.d[t][lcol + v] = make_float4(d, d, du, du);
-      }
-      if (kY) {
-        *reinterpret_cast<Raw*>(&sm.u[t][lcol]) = ru[i];
-        *reinterpret_cast<Raw*>(&sm.z[t][lcol]) = rz[i];
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < kBC; ++i) {
-      const int e = i * kThreads + tid;
-      if (e < kTT * kNs) {
-        const int n = e % kNs;
-        sm.bc[e / kNs][n / NPL][n % NPL] = to_f32(rb[i]);
-        if (kY) sm.bc[e / kNs][n / NPL][NPL + n % NPL] = to_f32(rc[i]);
-      }
-    }
-  };
-  auto flush = [&](int t0) {                                    // the tile of y to global memory
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int t = (i * kThreads + tid) / kRow;
-      if (t0 + t < t_end && c0 + lcol < a.C)
-        *reinterpret_cast<Raw*>((T*)a.y + ((int64_t)b * a.L + t0 + t) * a.C + c0 + lcol) = *reinterpret_cast<const Raw*>(&sm.u[t][lcol]);
-    }
-  };
-
-  if (t_begin < t_end) fetch(t_begin);
-  for (int t0 = t_begin; t0 < t_end; t0 += kTT) {
-    put(t0);
-    __syncthreads();
-    if (t0 + kTT < t_end) fetch(t0 + kTT);
+  for (int i = 0; i < tiles; ++i) {
+    Sm& sm = buf[i & 1];
+    const int t0 = t_begin + i * kTT;
+    barrier_sync(kFull + (i & 1));
     const int tokens = min(kTT, t_end - t0);
 #pragma unroll 1
     for (int t = 0; t < tokens; t += S) {                       // (kTT is a multiple of S; tokens past the end change nothing)
       float y[S];
 #pragma unroll
       for (int j = 0; j < S; ++j) {
-        const float4 q = sm.d[t + j][lc];
-        const float* bc = sm.bc[t + j][s];
+        const float2 q = sm.d[t + j][lc];
+        const typename Sm::Pack* bc = sm.bc[t + j][s];
         if (!kY) sum += q.x;
         if constexpr (NPL == 1) {
-          h[0] = fmaf(ex2(q.x * A2[0]), h[0], q.z * bc[0]);
+          h[0] = fmaf(ex2(q.x * A2[0]), h[0], q.y * bc[0]);
           if (kY) y[j] = h[0] * bc[1];
         } else {
           constexpr int kUse = kY ? 2 * NPL : NPL;              // B, and C
           float v[kUse];
+          constexpr int kWords = Sm::kPacked ? kUse / 2 : kUse;   // of 32 bits
+          uint32_t words[kWords];
 #pragma unroll
-          for (int n = 0; n < kUse; n += kUse % 4 ? 2 : 4) {
-            if constexpr (kUse % 4) {
-              const float2 x = *reinterpret_cast<const float2*>(bc + n);
-              v[n] = x.x; v[n + 1] = x.y;
+          for (int n = 0; n < kWords; n += kWords % 4 == 0 ? 4 : kWords % 2 == 0 ? 2 : 1) {
+            const uint32_t* at = reinterpret_cast<const uint32_t*>(bc) + n;
+            if constexpr (kWords % 4 == 0) {
+              const uint4 x = *reinterpret_cast<const uint4*>(at);
+              words[n] = x.x; words[n + 1] = x.y; words[n + 2] = x.z; words[n + 3] = x.w;
+            } else if constexpr (kWords % 2 == 0) {
+              const uint2 x = *reinterpret_cast<const uint2*>(at);
+              words[n] = x.x; words[n + 1] = x.y;
             } else {
-              const float4 x = *reinterpret_cast<const float4*>(bc + n);
-              v[n] = x.x; v[n + 1] = x.y; v[n + 2] = x.z; v[n + 3] = x.w;
+              words[n] = *at;
             }
           }
-          const uint64_t dd = pack2(q.x, q.y), du = pack2(q.z, q.w);
+#pragma unroll
+          for (int n = 0; n < kUse; ++n) {
+            if constexpr (Sm::kPacked) v[n] = __uint_as_float(n & 1 ? words[n / 2] & 0xffff0000u : words[n / 2] << 16);
+            else v[n] = __uint_as_float(words[n]);
+          }
+          const uint64_t dd = pack2(q.x, q.x), du = pack2(q.y, q.y);
           uint64_t yp = 0ull;
 #pragma unroll
           for (int n = 0; n < kPairs; ++n) {
@@ -279,8 +339,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_kernel(const ScanArgs a, int
         from_f32(&sm.u[t + s][lc], r);
       }
     }
-    __syncthreads();
-    if (kY) flush(t0);                                          // (a thread reads and refills the same places of u)
+    barrier_arrive(kDone + (i & 1));
   }
   if (c >= a.C) return;
 #pragma unroll
@@ -319,20 +378,20 @@ cudaError_t launch_tiles(const ScanArgs& a, const ScanPlan& p, void* ws, cudaStr
   const dim3 grid((unsigned)ceil_div(a.C, Sm::kCh), (unsigned)p.nchunk, (unsigned)a.B);
   static OncePerDevice opt_in;
   cudaError_t e = opt_in.run([] {
-    const cudaError_t r = cudaFuncSetAttribute(scan_kernel<T, S, NPL, WIDE, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Sm));
-    return r != cudaSuccess ? r : cudaFuncSetAttribute(scan_kernel<T, S, NPL, WIDE, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Sm));
+    const cudaError_t r = cudaFuncSetAttribute(scan_kernel<T, S, NPL, WIDE, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * (int)sizeof(Sm));
+    return r != cudaSuccess ? r : cudaFuncSetAttribute(scan_kernel<T, S, NPL, WIDE, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * (int)sizeof(Sm));
   });
   if (e != cudaSuccess) return e;
   float* state = p.nchunk > 1 ? (float*)((char*)ws + p.off_state) : nullptr;
   float* sum = p.nchunk > 1 ? (float*)((char*)ws + p.off_sum) : nullptr;
   if (p.nchunk > 1) {
-    e = launch_programmatic(scan_kernel<T, S, NPL, WIDE, false>, grid, kThreads, sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
+    e = launch_programmatic(scan_kernel<T, S, NPL, WIDE, false>, grid, kThreads + kStagers, 2 * sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
     if (e != cudaSuccess) return e;
     const int64_t n = (int64_t)a.B * a.C * a.Ns;
     e = launch_programmatic(scan_carry_kernel, dim3((unsigned)((n + 255) / 256)), 256, 0, st, a, p.nchunk, state, (const float*)sum);
     if (e != cudaSuccess) return e;
   }
-  return launch_programmatic(scan_kernel<T, S, NPL, WIDE, true>, grid, kThreads, sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
+  return launch_programmatic(scan_kernel<T, S, NPL, WIDE, true>, grid, kThreads + kStagers, 2 * sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
 }
 
 template <typename T, int S, int NPL>
