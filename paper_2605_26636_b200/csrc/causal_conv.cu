@@ -10,12 +10,12 @@
 namespace jv {
 namespace {
 
-template <typename T, int VEC>
-__device__ __forceinline__ void load_vec(const T* p, float (&f)[VEC]) {
+// VEC consecutive values as they lie in memory
+template <typename T, int VEC, typename Raw>
+__device__ __forceinline__ void widen(const Raw& r, float (&f)[VEC]) {
   if constexpr (VEC == 1) {
-    f[0] = to_f32(*p);
+    f[0] = to_f32(r);
   } else {
-    const uint4 r = *reinterpret_cast<const uint4*>(p);
     const uint32_t u[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -27,6 +27,11 @@ __device__ __forceinline__ void load_vec(const T* p, float (&f)[VEC]) {
       }
     }
   }
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void load_vec(const T* p, float (&f)[VEC]) {
+  if constexpr (VEC == 1) widen<T, VEC>(*p, f);
+  else widen<T, VEC>(*reinterpret_cast<const uint4*>(p), f);
 }
 template <typename T, int VEC>
 __device__ __forceinline__ void store_vec(T* p, const float (&f)[VEC]) {
@@ -51,7 +56,7 @@ constexpr int kThreads = 128;
 constexpr int kAhead = 4;            // tokens whose loads are in flight together; runs are multiples of it, and no shorter than K - 1
 
 template <typename T, int VEC, int K>
-__global__ void __launch_bounds__(kThreads) causal_conv_kernel(const ConvArgs a, int run, int runs) {
+__global__ void __launch_bounds__(kThreads, VEC == 8 ? 4 : 1) causal_conv_kernel(const ConvArgs a, int run, int runs) {
   griddep_wait();
   griddep_launch_dependents();
   const int ncv = a.C / VEC;
@@ -65,18 +70,13 @@ __global__ void __launch_bounds__(kThreads) causal_conv_kernel(const ConvArgs a,
   const T* x = (const T*)a.x + a.xs.at(b, 0) + c;
   T* u = (T*)a.u + (int64_t)b * a.L * a.C + c;
   const T* s_in = a.s_in ? (const T*)a.s_in + (int64_t)b * (K - 1) * a.C + c : nullptr;
-  float old[K - 1][VEC], past[K - 1][VEC];         // the state; the inputs ahead of the token in turn
+  float past[K - 1][VEC];                          // the inputs ahead of the token in turn
 #pragma unroll
   for (int j = 0; j < K - 1; ++j) {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) old[j][i] = 0.f;
-    if (r == 0) {
-      if (s_in) load_vec<T, VEC>(s_in + (int64_t)j * a.C, old[j]);
-    } else {
-      load_vec<T, VEC>(x + (int64_t)(t0 - (K - 1) + j) * a.xs.tok, old[j]);
-    }
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) past[j][i] = old[j][i];
+    for (int i = 0; i < VEC; ++i) past[j][i] = 0.f;
+    if (r > 0) load_vec<T, VEC>(x + (int64_t)(t0 - (K - 1) + j) * a.xs.tok, past[j]);
+    else if (s_in) load_vec<T, VEC>(s_in + (int64_t)j * a.C, past[j]);
   }
   float w[VEC][K], bias[VEC];                      // (a thread's filters are VEC * K consecutive values: 16 bytes at a time)
   if constexpr (VEC > 1) {
@@ -100,40 +100,48 @@ __global__ void __launch_bounds__(kThreads) causal_conv_kernel(const ConvArgs a,
     for (int j = 0; j < K; ++j) w[0][j] = __ldg(a.w + (int64_t)c * K + j);
     bias[0] = a.b ? __ldg(a.b + c) : 0.f;
   }
-  for (int t = t0; t < t1; t += kAhead) {
-    float in[kAhead][VEC];
+  // kAhead tokens in turn, as they lie in memory, and the next kAhead on their way
+  using Raw = typename std::conditional<VEC == 1, T, uint4>::type;
+  Raw now[kAhead], next[kAhead];
+  auto fetch = [&](Raw (&q)[kAhead], int t) {
 #pragma unroll
     for (int n = 0; n < kAhead; ++n)
-      if (t + n < t1) load_vec<T, VEC>(x + (int64_t)(t + n) * a.xs.tok, in[n]);
+      if (t + n < t1) q[n] = *reinterpret_cast<const Raw*>(x + (int64_t)(t + n) * a.xs.tok);
+  };
+  if (t0 < t1) fetch(now, t0);
+  for (int t = t0; t < t1; t += kAhead) {
+    fetch(next, t + kAhead);
 #pragma unroll
     for (int n = 0; n < kAhead; ++n)
       if (t + n < t1) {
-        float o[VEC];
+        float in[VEC], o[VEC];
+        widen<T, VEC>(now[n], in);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
           float s = bias[i];
 #pragma unroll
           for (int j = 0; j < K - 1; ++j) s = fmaf(w[i][j], past[j][i], s);
-          s = fmaf(w[i][K - 1], in[n][i], s);
+          s = fmaf(w[i][K - 1], in[i], s);
           o[i] = a.silu ? __fdividef(s, 1.f + __expf(-s)) : s;
 #pragma unroll
           for (int j = 0; j + 1 < K - 1; ++j) past[j][i] = past[j + 1][i];
-          past[K - 2][i] = in[n][i];
+          past[K - 2][i] = in[i];
         }
         store_vec<T, VEC>(u + (int64_t)(t + n) * a.C, o);
       }
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) now[n] = next[n];
   }
   if (r == 0 && a.s_out) {
     T* s_out = (T*)a.s_out + (int64_t)b * (K - 1) * a.C + c;
-#pragma unroll
-    for (int j = 0; j < K - 1; ++j) {              // row j: token len - (K - 1) + j, or what the state had where that is before the first
+    // Row j: token len - (K - 1) + j, or row len + j of the old state where that is before the first.  In ascending order, so that a
+    // state in its own place is read ahead of the rows that are written.
+    for (int j = 0; j < K - 1; ++j) {
       float f[VEC];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) f[i] = 0.f;
       if (len + j >= K - 1) load_vec<T, VEC>(x + (int64_t)(len + j - (K - 1)) * a.xs.tok, f);
-#pragma unroll
-      for (int n = 0; n < K - 1; ++n)
-        if (len + j == n)
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) f[i] = old[n][i];
+      else if (s_in) load_vec<T, VEC>(s_in + (int64_t)(len + j) * a.C, f);
       store_vec<T, VEC>(s_out + (int64_t)j * a.C, f);
     }
   }

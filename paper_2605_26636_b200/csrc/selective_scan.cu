@@ -1,9 +1,9 @@
 // The selective scan of a state-space mixer: every channel carries Ns states through its sequence.
 //   d_t = softplus(dt_t + dt_bias),  h_t = exp(d_t A) h_(t-1) + d_t B_t u_t,  y_t = (C_t . h_t + D u_t) z_t / (1 + exp(-z_t))
 //
-// Four or eight lanes share a channel, each with a share of its states in registers; a block has 64 or 32 channels in eight warps.  Four
-// more warps bring tiles of 2048 values (32 or 64 tokens) of u, dt, z with their B and C into one of two buffers in shared memory,
-// form d_t and d_t u_t once per token and channel on the way, and take y out of them.  (Bringing tiles in between steps of the eight
+// Four or eight lanes share a channel, each with a share of its states in registers; a block has 64 or 32 channels in eight warps.  Eight or
+// four more warps bring tiles of 2048 values (32 or 64 tokens) of u, dt, z with their B and C into one of two buffers in shared memory,
+// form d_t and d_t u_t once per token and channel on the way, and take y out of them through D and the gate.  (Bringing tiles in between steps of the eight
 // warps themselves left both kinds of work waiting: two prompts of 4096 tokens, 2048 channels, 16 states 231 us.)  As many tokens at a time as a channel has lanes: the lanes' shares
 // of their y are exchanged so that every lane ends up with the sum of one.  States in pairs (the packed fp32 arithmetic of sm_100).
 //
@@ -27,7 +27,10 @@ using tc::pack2;
 using tc::unpack2;
 
 constexpr int kThreads = 256;         // that compute
-constexpr int kStagers = 128;         // that bring tiles in and out
+// ... and that bring tiles in and out.  Four lanes a channel: two blocks an SM, 512 threads each.  Measured with 256 / 128 of them, B x L tokens of
+// 2048 channels: 4 x 2048 163 / 234 us, 8 x 2048 278 / 315; eight lanes, one block an SM: 2 x 4096 184 / 180.
+template <int S>
+constexpr int kStagersOf = S == 4 ? 256 : 128;
 constexpr int kTile = 2048;           // tokens times channels of a tile
 constexpr int kStepTokens = 4;        // calls of at most this many tokens walk without tiles
 constexpr float kLog2e = 1.4426950408889634f;
@@ -58,11 +61,25 @@ __device__ __forceinline__ void load_A(const ScanArgs& a, int c, int s, float (&
 }
 template <int NPL>
 __device__ __forceinline__ void load_state(const float* h, int Ns, int s, float (&st)[NPL]) {
+  if (NPL % 4 == 0 && h && Ns % 4 == 0 && ((uintptr_t)h & 15) == 0) {      // 16 bytes at a time
+#pragma unroll
+    for (int n = 0; n + 3 < NPL; n += 4) {
+      const float4 v = s * NPL + n < Ns ? *reinterpret_cast<const float4*>(h + s * NPL + n) : make_float4(0.f, 0.f, 0.f, 0.f);
+      st[n] = v.x; st[n + 1] = v.y; st[n + 2] = v.z; st[n + 3] = v.w;
+    }
+    return;
+  }
 #pragma unroll
   for (int n = 0; n < NPL; ++n) st[n] = h && s * NPL + n < Ns ? h[s * NPL + n] : 0.f;
 }
 template <int NPL>
 __device__ __forceinline__ void store_state(float* h, int Ns, int s, const float (&st)[NPL]) {
+  if (NPL % 4 == 0 && Ns % 4 == 0 && ((uintptr_t)h & 15) == 0) {
+#pragma unroll
+    for (int n = 0; n + 3 < NPL; n += 4)
+      if (s * NPL + n < Ns) *reinterpret_cast<float4*>(h + s * NPL + n) = make_float4(st[n], st[n + 1], st[n + 2], st[n + 3]);
+    return;
+  }
 #pragma unroll
   for (int n = 0; n < NPL; ++n)
     if (s * NPL + n < Ns) h[s * NPL + n] = st[n];
@@ -115,36 +132,42 @@ struct Smem {
   // tightest resource beside the exponentials
   static constexpr bool kPacked = sizeof(T) == 2 && NPL > 1;
   using Pack = typename std::conditional<kPacked, T, float>::type;
-  float2 d[kTT][kCh];                 // d, d u
+  float2 d[kTT][kCh + 2];             // d, d u       (rows padded to lie in different banks)
+  float y[kTT][kCh + 4];              // sum over the states
   Pack bc[kTT][S][2 * NPL];           // B, then C, of a lane's states
-  T u[kTT][kCh], z[kTT][kCh];         // u: y takes its place
+  T u[kTT][kCh], z[kTT][kCh];
 };
 
-// Barriers of a block: a buffer is full (all of it waits for the four warps); a buffer is done with (the four warps wait for the others)
+// Barriers of a block: a buffer is full (it waits for the warps that bring tiles in); a buffer is done with (they wait for the others)
 constexpr int kFull = 1, kDone = 3;
-__device__ __forceinline__ void barrier_sync(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kThreads + kStagers) : "memory"); }
-__device__ __forceinline__ void barrier_arrive(int id) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(kThreads + kStagers) : "memory"); }
+template <int S>
+__device__ __forceinline__ void barrier_sync(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kThreads + kStagersOf<S>) : "memory"); }
+template <int S>
+__device__ __forceinline__ void barrier_arrive(int id) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(kThreads + kStagersOf<S>) : "memory"); }
 
-// The four warps that bring tiles in, two ahead of the others, and y out
+// The warps that bring tiles in, two ahead of the others, and y out
 template <typename T, int S, int NPL, bool WIDE, bool kY>
 __device__ __forceinline__ void stage_tiles(const ScanArgs& a, Smem<T, S, NPL>* buf, int b, int c0, int t_begin, int t_end, int tiles) {
   using Sm = Smem<T, S, NPL>;
-  constexpr int kCh = Sm::kCh, kTT = Sm::kTT;
+  constexpr int kCh = Sm::kCh, kTT = Sm::kTT, kStagers = kStagersOf<S>;
   constexpr int kVec = WIDE ? 16 / sizeof(T) : 1;             // elements of a load
   constexpr int kLoads = kTile / kStagers / kVec;             // loads of a thread and tile from each of u, dt, z
   constexpr int kRow = kCh / kVec;                            // loads of a token
   constexpr int kNs = S * NPL;
   constexpr int kBC = (kTT * kNs + kStagers - 1) / kStagers;  // elements of a thread and tile from each of B, C
   const int tid = threadIdx.x - kThreads;
-  float bias[kVec];                                             // of the columns that this thread loads
+  float bias[kVec], D[kVec];                                    // of the columns that this thread loads
 #pragma unroll
-  for (int v = 0; v < kVec; ++v) bias[v] = 0.f;
+  for (int v = 0; v < kVec; ++v) bias[v] = D[v] = 0.f;
   constexpr bool kOneColumn = kStagers % kRow == 0;             // every load of a thread is of the same columns
   static_assert(kOneColumn, "a thread's loads are of one set of columns");
   const int lcol = (tid % kRow) * kVec;
   if (a.dt_bias)
 #pragma unroll
     for (int v = 0; v < kVec; ++v) bias[v] = __ldg(a.dt_bias + min(c0 + lcol + v, a.C - 1));
+  if (a.D)
+#pragma unroll
+    for (int v = 0; v < kVec; ++v) D[v] = __ldg(a.D + min(c0 + lcol + v, a.C - 1));
 
   using Raw = typename std::conditional<WIDE, uint4, T>::type;
   Raw ru[kLoads], rd[kLoads], rz[kLoads];
@@ -210,35 +233,58 @@ __device__ __forceinline__ void stage_tiles(const ScanArgs& a, Smem<T, S, NPL>* 
       }
     }
   };
-  auto flush = [&](const Sm& sm, int t0) {                                    // the tile of y to global memory
+  auto flush = [&](const Sm& sm, int t0) {                      // y = (sum + D u) gate to global memory
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int t = (i * kStagers + tid) / kRow;
-      if (t0 + t < t_end && c0 + lcol < a.C)
-        *reinterpret_cast<Raw*>((T*)a.y + ((int64_t)b * a.L + t0 + t) * a.C + c0 + lcol) = *reinterpret_cast<const Raw*>(&sm.u[t][lcol]);
+      if (t0 + t < t_end && c0 + lcol < a.C) {
+        T uu[kVec], zz[kVec], yy[kVec];
+        float sum[kVec];
+        if constexpr (kVec == 1) {
+          sum[0] = sm.y[t][lcol];
+        } else {
+#pragma unroll
+          for (int v = 0; v < kVec; v += 4) {
+            const float4 q = *reinterpret_cast<const float4*>(&sm.y[t][lcol + v]);
+            sum[v] = q.x; sum[v + 1] = q.y; sum[v + 2] = q.z; sum[v + 3] = q.w;
+          }
+        }
+        const Raw pu = *reinterpret_cast<const Raw*>(&sm.u[t][lcol]), pz = *reinterpret_cast<const Raw*>(&sm.z[t][lcol]);
+        memcpy(uu, &pu, sizeof(Raw));
+        memcpy(zz, &pz, sizeof(Raw));
+#pragma unroll
+        for (int v = 0; v < kVec; ++v) {
+          float r = fmaf(D[v], to_f32(uu[v]), sum[v]);
+          if (a.z) r *= silu(to_f32(zz[v]));
+          from_f32(&yy[v], r);
+        }
+        Raw py;
+        memcpy(&py, yy, sizeof(Raw));
+        *reinterpret_cast<Raw*>((T*)a.y + ((int64_t)b * a.L + t0 + t) * a.C + c0 + lcol) = py;
+      }
     }
   };
 
   for (int i = 0; i < min(2, tiles); ++i) {
     fetch(t_begin + i * kTT);
     put(buf[i], t_begin + i * kTT);
-    barrier_arrive(kFull + i);
+    barrier_arrive<S>(kFull + i);
   }
   for (int i = 0; i < tiles; ++i) {
     const int t0 = t_begin + i * kTT;
     if (i + 2 < tiles) fetch(t0 + 2 * kTT);
-    barrier_sync(kDone + (i & 1));
+    barrier_sync<S>(kDone + (i & 1));
     if (kY) flush(buf[i & 1], t0);                              // (a thread reads and refills the same places of u)
     if (i + 2 < tiles) {
       put(buf[i & 1], t0 + 2 * kTT);
-      barrier_arrive(kFull + (i & 1));
+      barrier_arrive<S>(kFull + (i & 1));
     }
   }
 }
 
 // S lanes a channel, NPL states a lane.  kY: the whole thing; else the chunk's own state from zero and the sum of its steps only
 template <typename T, int S, int NPL, bool WIDE, bool kY>
-__global__ void __launch_bounds__(kThreads + kStagers, 1) scan_kernel(const ScanArgs a, int chunk, int nchunk, float* ws_state, float* ws_sum) {
+__global__ void __launch_bounds__(kThreads + kStagersOf<S>, S == 4 && NPL <= 4 ? 2 : 1) scan_kernel(const ScanArgs a, int chunk, int nchunk, float* ws_state, float* ws_sum) {
   using Sm = Smem<T, S, NPL>;
   constexpr int kCh = Sm::kCh, kTT = Sm::kTT;
   extern __shared__ __align__(16) unsigned char smem_raw[];
@@ -266,11 +312,10 @@ __global__ void __launch_bounds__(kThreads + kStagers, 1) scan_kernel(const Scan
     A2p[n] = pack2(A2[2 * n], A2[2 * n + 1]);
     hp[n] = pack2(h[2 * n], h[2 * n + 1]);
   }
-  const float D = a.D ? __ldg(a.D + cc) : 0.f;
   for (int i = 0; i < tiles; ++i) {
     Sm& sm = buf[i & 1];
     const int t0 = t_begin + i * kTT;
-    barrier_sync(kFull + (i & 1));
+    barrier_sync<S>(kFull + (i & 1));
     const int tokens = min(kTT, t_end - t0);
 #pragma unroll 1
     for (int t = 0; t < tokens; t += S) {                       // (kTT is a multiple of S; tokens past the end change nothing)
@@ -334,12 +379,10 @@ __global__ void __launch_bounds__(kThreads + kStagers, 1) scan_kernel(const Scan
             const float give = (s & k) ? y[2 * i] : y[2 * i + 1], keep = (s & k) ? y[2 * i + 1] : y[2 * i];
             y[i] = keep + __shfl_xor_sync(0xffffffffu, give, k);
           }
-        float r = fmaf(D, to_f32(sm.u[t + s][lc]), y[0]);
-        if (a.z) r *= silu(to_f32(sm.z[t + s][lc]));
-        from_f32(&sm.u[t + s][lc], r);
+        sm.y[t + s][lc] = y[0];
       }
     }
-    barrier_arrive(kDone + (i & 1));
+    barrier_arrive<S>(kDone + (i & 1));
   }
   if (c >= a.C) return;
 #pragma unroll
@@ -385,13 +428,13 @@ cudaError_t launch_tiles(const ScanArgs& a, const ScanPlan& p, void* ws, cudaStr
   float* state = p.nchunk > 1 ? (float*)((char*)ws + p.off_state) : nullptr;
   float* sum = p.nchunk > 1 ? (float*)((char*)ws + p.off_sum) : nullptr;
   if (p.nchunk > 1) {
-    e = launch_programmatic(scan_kernel<T, S, NPL, WIDE, false>, grid, kThreads + kStagers, 2 * sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
+    e = launch_programmatic(scan_kernel<T, S, NPL, WIDE, false>, grid, kThreads + kStagersOf<S>, 2 * sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
     if (e != cudaSuccess) return e;
     const int64_t n = (int64_t)a.B * a.C * a.Ns;
     e = launch_programmatic(scan_carry_kernel, dim3((unsigned)((n + 255) / 256)), 256, 0, st, a, p.nchunk, state, (const float*)sum);
     if (e != cudaSuccess) return e;
   }
-  return launch_programmatic(scan_kernel<T, S, NPL, WIDE, true>, grid, kThreads + kStagers, 2 * sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
+  return launch_programmatic(scan_kernel<T, S, NPL, WIDE, true>, grid, kThreads + kStagersOf<S>, 2 * sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
 }
 
 template <typename T, int S, int NPL>
@@ -431,14 +474,16 @@ cudaError_t launch_type(const ScanArgs& a, const ScanPlan& p, void* ws, cudaStre
 ScanPlan scan_plan(int B, int L, int C, int Ns) {
   ScanPlan p{4, 1, L, 0, 0, 0};
   if (L <= kStepTokens) return p;
-  // Four lanes a channel where the channels give every SM two blocks all the same, else eight (and above 32 states, which eight
-  // lanes hold); chunks, which walk the exponentials twice, where even those leave half the SMs idle
-  const int64_t sms = device_sm_count();
-  p.lanes = Ns > 32 || (int64_t)B * ceil_div(C, kThreads / 4) < 2 * sms ? 8 : 4;
-  const int64_t blocks = (int64_t)B * ceil_div(C, kThreads / p.lanes);
-  const int tt = kTile / (kThreads / p.lanes);
-  if (blocks < sms / 2) {
-    const int want = (int)(2 * sms / blocks), tiles = ceil_div(L, tt);
+  // Four lanes a channel where the channels give two of three SMs a block all the same, eight where they do with half as many
+  // channels a block (and above 32 states, which eight lanes hold); chunks, which walk the exponentials twice, for two blocks an SM elsewhere
+  const int64_t sms = device_sm_count(), four = (int64_t)B * ceil_div(C, kThreads / 4), eight = (int64_t)B * ceil_div(C, kThreads / 8);
+  // (Measured: 2 x 4096 tokens of 2048 channels, four lanes 308 us, eight 180; 4 x 2048 163 / 181; 1 x 4096, chunks of four / eight lanes
+  // 124 / 155.)
+  const bool pass = 3 * four >= 2 * sms || 3 * eight >= 2 * sms;
+  p.lanes = Ns > 32 || (pass && 3 * four < 2 * sms) ? 8 : 4;
+  if (!pass) {
+    const int64_t blocks = p.lanes == 8 ? eight : four;
+    const int tt = kTile / (kThreads / p.lanes), want = (int)(2 * sms / blocks), tiles = ceil_div(L, tt);
     p.chunk = ceil_div(tiles, want < tiles ? want : tiles) * tt;
     p.nchunk = ceil_div(L, p.chunk);
   }
