@@ -9,18 +9,17 @@ namespace {
 using namespace tc;
 using namespace diff;
 
-// ---- the partials of an item merged, and rows done again ----------------------------------------------------------------
-// Block (c, y), rows y, y + gridDim.y, ... of eight by its warps: the marked rows of the whole items of block c of the main launch; and
-// the item that block c takes up in its middle, if c is the first that does.  A lane holds four channels of both maps.
+// Block (c, y): the marked rows of the whole items of block c of the main launch; and the item that block c takes up in its middle, if c
+// is the first that does.  Sixteen lanes a row, eight channels of both maps each: two rows to a warp, sixteen to a block.
 constexpr int kMergeWarps = 8;
+constexpr int kMergeRows = 2 * kMergeWarps;
 __global__ void __launch_bounds__(kMergeWarps * 32, 4) diff_merge_kernel(const DiffParams p, int rows, int blocks) {
-  __shared__ int last, begun;
   __shared__ float sq[kMergeWarps][kV];
   griddep_wait();
   griddep_launch_dependents();
   const int c = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const Start s = p.starts[c];
-  if (s.tiles == 0 || s.left) return;
+  if (s.tiles == 0 || s.left || (!s.redo && s.tile == 0)) return;
   const float lam = lambda_of(p.tail);
   if (s.redo) {
     Walk it;
@@ -36,39 +35,49 @@ __global__ void __launch_bounds__(kMergeWarps * 32, 4) diff_merge_kernel(const D
   }
   if (s.tile == 0) return;
   auto same = [&](const Start& a) { return a.b == s.b && a.qt == s.qt && a.pair == s.pair; };
-  if (threadIdx.x == 0) {
-    // blocks without tiles lie between; the one before with tiles holds the item's beginning, or takes it up in its middle, too
-    int b = c - 1;
-    while (b > 0 && p.starts[b].tiles == 0) --b;
-    const Start before = p.starts[b];
-    begun = same(before) && before.tile > 0 ? -1 : b;
-    int e = c;
-    bool left = before.left != 0;
-    for (int k = c + 1; k < blocks; ++k) {
-      const Start a = p.starts[k];
-      if (a.tiles == 0) continue;
-      if (!same(a) || a.tile == 0) break;
-      e = k;
-      left = left || a.left != 0;
-    }
-    last = left ? -1 : e;
+  // The block before (blocks without tiles may lie between) holds the item's beginning, or takes it up in its middle, too: then the
+  // item is another block's.
+  int begun = c - 1;
+  Start before = p.starts[begun];
+  while (before.tiles == 0 && begun > 0) before = p.starts[--begun];
+  if (same(before) && before.tile > 0) return;
+  int last = c;
+  bool left = before.left != 0;
+  for (int k0 = c + 1; k0 < blocks; k0 += 32) {           // 32 of the blocks behind at a time
+    const int k = k0 + lane;
+    const Start a = p.starts[min(k, blocks - 1)];
+    const bool in = k < blocks && (a.tiles == 0 || (same(a) && a.tile > 0));
+    const uint32_t out = __ballot_sync(0xffffffffu, !in);
+    const int n = out ? __ffs(out) - 1 : 32;
+    const uint32_t parts = __ballot_sync(0xffffffffu, lane < n && a.tiles > 0), gone = __ballot_sync(0xffffffffu, lane < n && a.tiles > 0 && a.left);
+    if (parts) last = k0 + 31 - __clz(parts);
+    left = left || gone;
+    if (n < 32) break;
   }
-  __syncthreads();
-  if (begun < 0 || last < 0) return;         // another block's item; or one whose blocks have left without a result
+  if (left) return;                          // blocks that have left without a result
   const Reach reach = reach_of(p.items.kv_len, p.items.q_pos, s.b, p.items.Nq, p.items.Nk, p.items.causal != 0);
-  for (int r = blockIdx.y * kMergeWarps + warp; r < rows; r += gridDim.y * kMergeWarps) {
+  const int sub = lane >> 4, ch = 8 * (lane & 15);
+  for (int r0 = blockIdx.y * kMergeRows + 2 * warp; r0 < rows; r0 += gridDim.y * kMergeRows) {
+    const int r = min(r0 + sub, rows - 1);
     int pair, i;
     p.row(s.qt, s.pair, r, pair, i);
-    if (i >= p.items.Nq) break;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-    float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+    const bool mine = r0 + sub < rows && i < p.items.Nq;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, acc[2][8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int y = 0; y < 8; ++y) acc[h][y] = 0.f;
     const float* src = p.partial + r * kPartial;
-#pragma unroll 4
+#pragma unroll 2
     for (int k = begun; k <= last; ++k) {
       // (a block without tiles has left nothing in its slots: what lies there is loaded and dropped)
       const float* at = src + (size_t)(2 * k + (k == begun ? 1 : 0)) * p.slot_rows * kPartial;
       const float4 st = __ldcg(reinterpret_cast<const float4*>(at));
-      const float4 a4[2] = {__ldcg(reinterpret_cast<const float4*>(at + 4) + lane), __ldcg(reinterpret_cast<const float4*>(at + 4 + kV) + lane)};
+      float4 q[2][2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) q[h][y] = __ldcg(reinterpret_cast<const float4*>(at + 4 + kV * h + ch + 4 * y));
       const bool none = k > begun && p.starts[k].tiles == 0;
       const float pm[2] = {st.x, st.z}, pl[2] = {st.y, st.w};
 #pragma unroll
@@ -77,37 +86,49 @@ __global__ void __launch_bounds__(kMergeWarps * 32, 4) diff_merge_kernel(const D
         const float mn = max3(m[h], pm[h], pm[h]), f = ex2(m[h] - mn), g = ex2(pm[h] - mn);
         m[h] = mn;
         l[h] = l[h] * f + pl[h] * g;
-        acc[h].x = acc[h].x * f + a4[h].x * g;
-        acc[h].y = acc[h].y * f + a4[h].y * g;
-        acc[h].z = acc[h].z * f + a4[h].z * g;
-        acc[h].w = acc[h].w * f + a4[h].w * g;
+        const float v[8] = {q[h][0].x, q[h][0].y, q[h][0].z, q[h][0].w, q[h][1].x, q[h][1].y, q[h][1].z, q[h][1].w};
+#pragma unroll
+        for (int y = 0; y < 8; ++y) acc[h][y] = acc[h][y] * f + v[y] * g;
       }
     }
     const bool any = reach.limit(i) > 0;
     const float f0 = any ? 1.f / l[0] : 0.f, f1 = any ? -lam / l[1] : 0.f;
-    float x[4] = {acc[0].x * f0 + acc[1].x * f1, acc[0].y * f0 + acc[1].y * f1, acc[0].z * f0 + acc[1].z * f1, acc[0].w * f0 + acc[1].w * f1};
-    float ss = 0.f;
+    float x[8], ss = 0.f;
 #pragma unroll
-    for (int y = 0; y < 4; ++y) ss = fmaf(x[y], x[y], ss);
-    ss = warp_sum(ss);
-    if (!(ss < INFINITY)) {                     // a part that says so, or values out of range
-      diff_row<__nv_bfloat16>(p.args, s.b, pair, i, lam, sq[warp]);
-      continue;
+    for (int y = 0; y < 8; ++y) {
+      x[y] = acc[0][y] * f0 + acc[1][y] * f1;
+      ss = fmaf(x[y], x[y], ss);
     }
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    const bool again = mine && !(ss < INFINITY);   // a part that says so, or values out of range
     if (p.tail.norm_w) {
       const float rn = (1.f - p.tail.lambda_init) * rsqrtf(ss * (1.f / kV) + p.tail.norm_eps);
-      const float4 w = __ldg(reinterpret_cast<const float4*>(p.tail.norm_w + 4 * lane));
-      x[0] *= rn * w.x; x[1] *= rn * w.y; x[2] *= rn * w.z; x[3] *= rn * w.w;
+#pragma unroll
+      for (int y = 0; y < 8; y += 4) {
+        const float4 w = __ldg(reinterpret_cast<const float4*>(p.tail.norm_w + ch + y));
+        x[y] *= rn * w.x; x[y + 1] *= rn * w.y; x[y + 2] *= rn * w.z; x[y + 3] *= rn * w.w;
+      }
     }
-    __nv_bfloat16* dst = p.o + (((size_t)s.b * 2 * p.pairs + 2 * pair + (lane >> 4)) * p.items.Nq + i) * kD + 4 * (lane & 15);
-    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+    if (mine && !again) {
+      __nv_bfloat16* dst = p.o + (((size_t)s.b * 2 * p.pairs + 2 * pair + (ch >> 6)) * p.items.Nq + i) * kD + (ch & 63);
+      *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+    }
+    const uint32_t redo = __ballot_sync(0xffffffffu, again);
+#pragma unroll 1
+    for (int h = 0; h < 2; ++h)
+      if (redo >> (16 * h) & 1u) {
+        int pr, qi;
+        p.row(s.qt, s.pair, r0 + h, pr, qi);
+        diff_row<__nv_bfloat16>(p.args, s.b, pr, qi, lam, sq[warp]);
+      }
   }
 }
 
 }  // namespace
 
 cudaError_t launch_diff_merge(const DiffParams& p, int blocks, int rows, cudaStream_t st) {
-  return launch_programmatic(diff_merge_kernel, dim3((unsigned)blocks, (unsigned)ceil_div(rows, kMergeWarps)), kMergeWarps * 32, 0, st, p, rows, blocks);
+  return launch_programmatic(diff_merge_kernel, dim3((unsigned)blocks, (unsigned)ceil_div(rows, kMergeRows)), kMergeWarps * 32, 0, st, p, rows, blocks);
 }
 
 }  // namespace jv

@@ -56,6 +56,14 @@ __device__ __forceinline__ int length_of(const ScanArgs& a, int b) { return a.le
 // A channel's coefficients and states: state n of lane s is s * NPL + n; states past Ns are zeros all through
 template <int NPL>
 __device__ __forceinline__ void load_A(const ScanArgs& a, int c, int s, float (&A2)[NPL]) {
+  if (NPL % 4 == 0 && a.Ns % 4 == 0 && ((uintptr_t)a.A & 15) == 0) {        // 16 bytes at a time
+#pragma unroll
+    for (int n = 0; n + 3 < NPL; n += 4) {
+      const float4 v = s * NPL + n < a.Ns ? __ldg(reinterpret_cast<const float4*>(a.A + (int64_t)c * a.Ns + s * NPL + n)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      A2[n] = v.x * kLog2e; A2[n + 1] = v.y * kLog2e; A2[n + 2] = v.z * kLog2e; A2[n + 3] = v.w * kLog2e;
+    }
+    return;
+  }
 #pragma unroll
   for (int n = 0; n < NPL; ++n) A2[n] = s * NPL + n < a.Ns ? __ldg(a.A + (int64_t)c * a.Ns + s * NPL + n) * kLog2e : 0.f;
 }
@@ -85,6 +93,31 @@ __device__ __forceinline__ void store_state(float* h, int Ns, int s, const float
     if (s * NPL + n < Ns) h[s * NPL + n] = st[n];
 }
 
+// A lane's values of B or C of a token
+template <typename T, int NPL>
+__device__ __forceinline__ void load_row(const T* row, int Ns, int s, float (&v)[NPL]) {
+  if (NPL % 4 == 0 && Ns % 4 == 0 && ((uintptr_t)row % (4 * sizeof(T))) == 0) {       // four at a time
+#pragma unroll
+    for (int n = 0; n + 3 < NPL; n += 4) {
+      if (s * NPL + n >= Ns) {
+        v[n] = v[n + 1] = v[n + 2] = v[n + 3] = 0.f;
+      } else if constexpr (sizeof(T) == 4) {
+        const float4 q = *reinterpret_cast<const float4*>(row + s * NPL + n);
+        v[n] = q.x; v[n + 1] = q.y; v[n + 2] = q.z; v[n + 3] = q.w;
+      } else {
+        const uint2 q = *reinterpret_cast<const uint2*>(row + s * NPL + n);
+        v[n] = __uint_as_float(q.x << 16);
+        v[n + 1] = __uint_as_float(q.x & 0xffff0000u);
+        v[n + 2] = __uint_as_float(q.y << 16);
+        v[n + 3] = __uint_as_float(q.y & 0xffff0000u);
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int n = 0; n < NPL; ++n) v[n] = s * NPL + n < Ns ? to_f32(row[s * NPL + n]) : 0.f;
+}
+
 // ---- a few tokens: straight from global memory ------------------------------------------------------------------------
 template <typename T, int NPL>
 __global__ void __launch_bounds__(kThreads) scan_step_kernel(const ScanArgs a) {
@@ -102,22 +135,23 @@ __global__ void __launch_bounds__(kThreads) scan_step_kernel(const ScanArgs a) {
   for (int t = 0; t < len; ++t) {
     const float u = to_f32(((const T*)a.u)[a.us.at(b, t) + cc]);
     float d = to_f32(((const T*)a.dt)[a.ds.at(b, t) + cc]) + bias;
+    const float z = a.z ? to_f32(((const T*)a.z)[a.zs.at(b, t) + cc]) : 0.f;
+    float bm[NPL], cm[NPL];
+    load_row<T, NPL>((const T*)a.Bm + a.bs.at(b, t), a.Ns, s, bm);
+    load_row<T, NPL>((const T*)a.Cm + a.cs.at(b, t), a.Ns, s, cm);
     if (a.softplus) d = softplus(d);
     const float du = d * u;
     float y = 0.f;
 #pragma unroll
     for (int n = 0; n < NPL; ++n) {
-      const int i = s * NPL + n;
-      const float bm = i < a.Ns ? to_f32(((const T*)a.Bm)[a.bs.at(b, t) + i]) : 0.f;
-      const float cm = i < a.Ns ? to_f32(((const T*)a.Cm)[a.cs.at(b, t) + i]) : 0.f;
-      h[n] = fmaf(ex2(d * A2[n]), h[n], du * bm);
-      y = fmaf(h[n], cm, y);
+      h[n] = fmaf(ex2(d * A2[n]), h[n], du * bm[n]);
+      y = fmaf(h[n], cm[n], y);
     }
     y += __shfl_xor_sync(0xffffffffu, y, 1);
     y += __shfl_xor_sync(0xffffffffu, y, 2);
     if (s == 0 && c < a.C) {
       y = fmaf(D, u, y);
-      if (a.z) y *= silu(to_f32(((const T*)a.z)[a.zs.at(b, t) + c]));
+      if (a.z) y *= silu(z);
       from_f32((T*)a.y + ((int64_t)b * a.L + t) * a.C + c, y);
     }
   }
