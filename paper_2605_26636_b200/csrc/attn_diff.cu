@@ -472,7 +472,10 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (threadIdx.x == 0) p.starts[blockIdx.x].redo = bar->redo;
+  if (threadIdx.x == 0) {
+    p.starts[blockIdx.x].redo = bar->redo;
+    if (bar->abort_flag) p.starts[blockIdx.x].left = 1;   // a wait has run out: its partials are not to be merged
+  }
   if (warp == 0)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
 }

@@ -297,7 +297,10 @@ diff_rows_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant
       if (threadIdx.x == 0) sh->leave = sh->abort_flag;
       workers_sync();                         // (the other map's turn, or the next item's)
     }
-    if (sh->leave) break;                     // a wait has run out: no result of this item is complete
+    if (sh->leave) {                          // a wait has run out: no result of this item is complete, and none to be merged
+      if (threadIdx.x == 0) p.starts[blockIdx.x].left = 1;
+      break;
+    }
     if (!it.whole()) {
       if (tr >= rows) continue;
       float* dst = p.partial + ((size_t)partial_slot(blockIdx.x, it.t0) * kRows + tr) * kPartial;

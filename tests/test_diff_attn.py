@@ -192,6 +192,92 @@ def test_streams_capture_and_repeats(Nq, Nk):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("seed", range(10))
+def test_equal_shares_of_unequal_sequences(seed):
+    """Blocks take equal shares of all sequences' keys, cut wherever they come: many and few sequences, more of them than a block has
+    threads, lengths from none to all, several pairs, prompts and single tokens."""
+    g = torch.Generator().manual_seed(seed)
+    pick = lambda *a: a[int(torch.randint(len(a), (1,), generator=g))]
+    Nq, Hkv = pick(1, 1, 3, 150, 300), pick(2, 2, 4, 6)
+    H = Hkv * pick(1, 2)
+    B, Nk = ((pick(700, 900), 200) if seed < 2 else (pick(5, 11, 37), pick(130, 900, 1500)))
+    Nq = 1 if seed < 2 else Nq
+    q, k, v, lam, w = _tensors(B, H, Hkv, Nq, Nk, seed=seed)
+    lens = (torch.rand(B, generator=g) ** 2 * (Nk + 1)).int().cuda()
+    pos = (lens - torch.randint(0, Nq + 40, (B,), generator=g).cuda()).int()
+    _check(q, k, v, lam, w, kv_len=lens, rms=False)
+    _check(q, k, v, lam, None, causal=True, kv_len=lens, q_pos=pos, rms=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H,Nq,Nk", [(64, 256, 384), (2, 140, 3000), (2, 1, 3000), (300, 128, 256)])
+def test_scores_that_outgrow_the_first_keys(H, Nq, Nk):
+    """Scores far above, or below, those of the first 64 keys, and values too large to be squared: rows that are done again, of items that
+    one block has whole (many pairs) and of items in parts (few)."""
+    q, k, v, lam, w = _tensors(1, H, H, Nq, Nk, seed=3)
+    up = torch.ones(Nk)
+    up[:64] = 0.02
+    up[200:] = 8.0
+    kk = (k.float() * up[:, None].cuda()).to(k.dtype)
+    _check(8 * q, kk, v, lam, None, rms=False)                                   # maxima grow by some hundred
+    _check(8 * q, kk, v, lam, w, causal=Nq > 1, rms=False)
+    _check(8 * q, kk.flip(2), v, lam, w, rms=False)                              # and fall
+    some = q.clone()
+    some[:, :, ::3] *= 8                                                       # every third row only
+    _check(some, kk, v, lam, None, rms=False)
+    few = k.abs() * 2.0
+    few[:, :, :64] = -few[:, :, :64]
+    _check(4 * q.abs(), few, v, lam, None, rms=False)                            # first keys far below every other
+    first = few.clone()
+    first[:, :, :64] = -math.inf                                                # and such as weigh nothing
+    out = jv.diff_attn(4 * q.abs() + 1, first, v, lam, 0.8)
+    ref, bound = _reference(4 * q.abs() + 1, few[:, :, 64:], v[:, :, 64:], lam, 0.8, None, 1e-5, False, None, None, 0.0)
+    assert ((out.double() - ref).abs() <= HALF[q.dtype] * (ref.abs() + bound) + bound).all()
+    big = (v.float() * 1e22).to(v.dtype)                                       # (without a norm: its squares leave fp32)
+    o = jv.diff_attn(q, k, big, lam, 0.8)
+    ref, bound = _reference(q, k, big, lam, 0.8, None, 1e-5, False, None, None, 0.0)
+    assert ((o.double() - ref).abs() <= HALF[q.dtype] * (ref.abs() + bound) + bound).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("Nq", [1, 130])
+def test_calls_while_the_status_word_is_set(Nq):
+    q, k, v, lam, w = _tensors(3, 4, 4, Nq, 1700, seed=8)
+    call = lambda out: jv.diff_attn(q, k, v, lam, 0.8, norm_weight=w, out=out)
+    good = call(torch.empty_like(q))
+    assert jv.device_status() == jv.JV_OK
+    jv.selftest_wait_timeout(1000)
+    kept = call(torch.full_like(q, 1234.5))
+    torch.cuda.synchronize()
+    assert (kept == 1234.5).all()
+    assert jv.device_status() == jv.JV_ERR_TIMEOUT and jv.device_status() == jv.JV_OK
+    assert torch.equal(call(torch.empty_like(q)), good)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("Nq,dtype", [(1, torch.bfloat16), (140, torch.bfloat16), (3, torch.float32)])
+def test_a_cache_whose_offsets_pass_32_bits(Nq, dtype):
+    B, H, Nk, far = 3, 4, 333, (1 << 31) // 2 + 4096          # elements between batch elements: the third begins behind 2^31
+    q, k, v, lam, w = _tensors(B, H, H, Nq, Nk, dtype=dtype, seed=4)
+    pool = torch.empty(2 * far + 2 * H * Nk * 64, dtype=dtype, device="cuda")
+    ks = pool.as_strided((B, H, Nk, 64), (far, Nk * 64, 64, 1))
+    vs = pool.as_strided((B, H, Nk, 64), (far, Nk * 64, 64, 1), H * Nk * 64)
+    ks.copy_(k)
+    vs.copy_(v)
+    assert torch.equal(jv.diff_attn(q, ks, vs, lam, 0.8, norm_weight=w), jv.diff_attn(q, k, v, lam, 0.8, norm_weight=w))
+
+
+@pytest.mark.gpu
+def test_forced_generic_kernel():
+    q, k, v, lam, w = _tensors(2, 4, 2, 70, 150)
+    prev = jv.set_force_generic(True)
+    try:
+        _check(q, k, v, lam, w, causal=True)
+    finally:
+        jv.set_force_generic(prev)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("causal", [False, True])
 def test_between_norm_and_projections(causal):
     """norm -> QKV projection -> differential attention -> output projection, as a block runs them."""

@@ -145,6 +145,36 @@ def test_large_mean_constant_rows_and_values_that_are_none():
 
 
 @pytest.mark.gpu
+def test_rows_whose_offsets_pass_32_bits():
+    C, rows, far = 264, 40, 1 << 26                             # elements between rows: 2^31 behind the 32nd
+    x, dy, w, b = _inputs(rows, C, torch.bfloat16, seed=6)
+    pool = torch.empty(far * (rows - 1) + 2 * C, dtype=torch.bfloat16, device="cuda")
+    xs, ds = pool.as_strided((rows, C), (far, 1)), pool.as_strided((rows, C), (far, 1), C)
+    xs.copy_(x)
+    ds.copy_(dy)
+    stats = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    assert torch.equal(jv.layer_norm(xs, w, b, stats=stats), jv.layer_norm(x, w, b))
+    assert all(torch.equal(p, q) for p, q in zip(jv.layer_norm_grad(ds, xs, w, *stats), jv.layer_norm_grad(dy, x, w, *stats)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_many_rows(dtype):
+    """Enough rows for two to a warp, their count odd, and for several to a warp of the gradient."""
+    for rows, C in ((5001, 384), (9999, 1024), (7001, 129)):
+        x, dy, w, b = _inputs(rows, C, dtype, seed=7)
+        stats = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        out, check = guarded_empty((rows, C), dtype, "cuda")
+        y = jv.layer_norm(x, w, b, eps=1e-5, out=out, stats=stats)
+        check()
+        ref, bound, m, r = _reference(x, w, b, 1e-5)
+        assert ((y.double() - ref).abs() <= HALF[dtype] * (ref.abs() + bound) + bound).all()
+        assert ((stats[0].double() - m).abs() <= 64 * U * x.double().abs().mean(-1)).all()
+        one = [torch.cat([jv.layer_norm(x[i:i + 1], w, b, eps=1e-5) for i in (0, 1, rows - 1)])]
+        assert torch.equal(one[0], y[[0, 1, rows - 1]])               # however many rows a call has
+
+
+@pytest.mark.gpu
 def test_captured_and_on_another_stream():
     x, dy, w, b = _inputs(129, 384, torch.bfloat16, seed=4)
     y, dx = torch.empty_like(x), torch.empty_like(x)

@@ -185,6 +185,28 @@ def test_prompt_then_tokens():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("L", [1, 40])
+def test_sequences_whose_offsets_pass_32_bits(L):
+    B, C, Ns, far = 3, 72, 16, (1 << 31) // 2 + 64              # elements between batch elements: the third begins behind 2^31
+    i = _scan_inputs(B, L, C, Ns, torch.bfloat16)
+    pool = torch.empty(2 * far + 4096 * 8, dtype=torch.bfloat16, device="cuda")
+    place = lambda t, at: pool.as_strided(t.shape, (far, t.shape[2], 1), at * 4096).copy_(t)
+    moved = dict(i, **{n: place(i[n], at) for at, n in enumerate(("u", "dt", "z", "Bm", "Cm"))})
+    assert torch.equal(jv.selective_scan(**moved), jv.selective_scan(**i))
+    w = torch.randn(C, 4, device="cuda")
+    assert torch.equal(jv.causal_conv(moved["u"], w), jv.causal_conv(i["u"], w))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,L,C,Ns", [(3, 500, 2100, 16), (2, 300, 1024, 40), (1, 900, 100, 33)])
+def test_lanes_and_chunks(B, L, C, Ns):
+    """Four lanes a channel, eight, eight with chunks; channels that end within a block."""
+    for dtype in (torch.bfloat16, torch.float32):
+        lens = torch.tensor([L - 7 * b for b in range(B)], dtype=torch.int32, device="cuda")
+        _scan_check(_scan_inputs(B, L, C, Ns, dtype), dtype, lens)
+
+
+@pytest.mark.gpu
 def test_far_values_and_no_numbers():
     i = _scan_inputs(1, 40, 64, 16, torch.float32)
     big = dict(i, dt=torch.where(torch.rand_like(i["dt"]) < 0.1, 60.0, -90.0))     # steps of 60 (the state forgets all) and of nothing
