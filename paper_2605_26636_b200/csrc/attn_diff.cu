@@ -23,6 +23,10 @@
 // voted on by the whole warp, cost it 1300 clocks a step, whatever was left out of the arithmetic.  So one lane per role, three
 // issuers, and the softmax warps' looks at their barriers ahead of the arithmetic that hides them.
 //
+// The difference of the maps is smaller than either: bf16 probabilities left o at 2.6e-3 of the exact result (its own rounding: 1.7e-3).
+// So map 0, which weighs most, has its probabilities of kLoKeys of every 64 keys as two bf16 terms: what the rounding took off them
+// goes through shared memory (tensor memory is full) into products of their own, 2.3e-3.
+//
 // Behind an item's last key each of a row's four threads takes 32 channels from both accumulators: the sums and the shares of
 // the row's mean square are exchanged through shared memory, the difference is normalised and written.  Parts of an item (see
 // attn_diff.cuh) go to the workspace as they are.
@@ -49,6 +53,8 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kFirstSoftmaxWarp = 4;
 constexpr uint32_t kTmemCols = 512;
 constexpr int kSub = 64;                    // keys per step
+constexpr int kLoKeys = 32;                 // of them, the first, with a second term in map 0
+constexpr int kLoBytes = kTile * kLoKeys * 2;   // of a set: rows of 64 bytes, 64-byte swizzle
 constexpr float kFine = 1152921504606846976.f;   // 2^60: sums between this and its inverse are used as they are
 // Tensor-memory columns: scores of map m at 64 m, probabilities of set s at 128 + 32 s, O_m at 256 + 128 m
 constexpr uint32_t kColS = 0, kColP = 128, kColO = 256;
@@ -69,7 +75,8 @@ struct __align__(8) Barriers {
   int redo;
 };
 constexpr size_t kSmemTiles = (kQB + kKS + kVS) * (size_t)kTileBytes;          // 224 KB
-constexpr size_t kSmemBytes = kSmemTiles + sizeof(Barriers) + 1024;            // + alignment slack
+constexpr size_t kSmemLo = 2 * (size_t)kLoBytes;                               // the two sets of map 0
+constexpr size_t kSmemBytes = kSmemTiles + kSmemLo + sizeof(Barriers) + 1024;  // + alignment slack
 static_assert(kSmemBytes <= 227 * 1024, "shared memory of one block");
 
 constexpr uint32_t kIdescQK = idesc(kTile, kSub, 0);       // S = Q K^T: M128 N64, both operands K-major
@@ -78,6 +85,43 @@ constexpr uint32_t kIdescPV = idesc(kTile, kV, 1);         // O = P V: M128 N128
 // tcgen05.commit of everything this thread has issued, to be called by one lane
 __device__ __forceinline__ void commit_1(uint64_t* bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
+// Descriptor of a K-major operand in rows of 64 bytes, 64-byte swizzle (16-byte chunk c of row r at c ^ (r / 2 % 4)), 8-row groups 512
+// bytes apart; 32 bytes on per K step of 16
+__device__ __forceinline__ uint64_t smem_desc_64(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) /* LBO (unused) */ | (32ull << 32) /* SBO = 512 B */ |
+         (1ull << 46) /* descriptor version */ | (4ull << 61) /* SWIZZLE_64B */;
+}
+// p = exp2(s * sl2 + neg) for 32 scores; adds them into four packed partial sums and packs them to bf16 pairs (even key low).  lo: where
+// what the rounding takes off goes, this thread's row in four chunks of 16 bytes (chunk c at lo + 16 (c ^ turn)); null: nowhere.
+__device__ __forceinline__ void weights32(const uint32_t (&v)[32], uint64_t sl2x2, uint64_t neg2, uint64_t (&lsum)[4], uint32_t (&pk)[16],
+                                          unsigned char* lo, int turn) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    uint64_t pp[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int i = 4 * c + j;
+      float x0, x1;
+      unpack2(fma2(pack2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), sl2x2, neg2), x0, x1);
+      const float p0 = ex2(x0), p1 = ex2(x1);
+      pp[j] = pack2(p0, p1);
+      lsum[j] = add2(lsum[j], pp[j]);
+      pk[i] = pack_bf16(p0, p1);
+    }
+    if (lo) {
+      uint32_t r[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t h = pk[4 * c + j];
+        float r0, r1;
+        unpack2(add2(pp[j], pack2(-__uint_as_float(h << 16), -__uint_as_float(h & 0xffff0000u))), r0, r1);
+        r[j] = pack_bf16(r0, r1);
+      }
+      *reinterpret_cast<uint4*>(lo + 16 * (c ^ turn)) = make_uint4(r[0], r[1], r[2], r[3]);
+    }
+  }
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
@@ -90,8 +134,8 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
     prefetch_map(&mapV);
   }
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  Barriers* bar = reinterpret_cast<Barriers*>(smem + kSmemTiles);
-  const uint32_t sQ = smem_u32(smem), sK = sQ + kQB * kTileBytes, sV = sK + kKS * kTileBytes;
+  Barriers* bar = reinterpret_cast<Barriers*>(smem + kSmemTiles + kSmemLo);
+  const uint32_t sQ = smem_u32(smem), sK = sQ + kQB * kTileBytes, sV = sK + kKS * kTileBytes, sLo = sV + kVS * kTileBytes;
 
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
@@ -267,6 +311,12 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
 #pragma unroll
             for (int c = 0; c < kSub / 16; ++c)
               mma_ts_1(dO, dP + h * 32 + c * 8, desc_advance(dv, h * (kSub * kD * 2) + c * 2048), kIdescPV, c > 0 || h > 0 || j > it.t0 ? 1u : 0u);
+            if (x == 0) {
+              const uint64_t dl = smem_desc_64(sLo + h * kLoBytes);
+#pragma unroll
+              for (int c = 0; c < kLoKeys / 16; ++c)
+                mma_ss_1(dO, desc_advance(dl, c * 32), desc_advance(dv, h * (kSub * kD * 2) + c * 2048), kIdescPV, 1u);
+            }
             commit_1(&bar->pv_done[x][h]);
           }
           if (!ok) break;
@@ -291,6 +341,7 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
     const float sl2 = p.scale_log2;
     const uint64_t sl2x2 = pack2(sl2, sl2);
     const float lam = lambda_of(p.tail);
+    unsigned char* lo = x == 0 ? smem + kSmemTiles + hb * kLoBytes + r * (kLoKeys * 2) : nullptr;
     bool ok = true;
     uint32_t n = 0;                   // steps of this set so far: parity of its barriers
     uint32_t items = 0;               // items so far
@@ -354,24 +405,24 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
         const uint64_t neg2 = pack2(neg, neg);
         uint64_t lsum[4] = {0ull, 0ull, 0ull, 0ull};
         uint32_t pa[16], pb[16];
-        float unused[4];
-        exp32<false, 0>(va, sl2x2, neg2, lsum, pa, unused);
-        // a look, ahead of the second half, at whether P(u - 2) has been read
-        const bool room = n == 0 || __all_sync(0xffffffffu, mbar_test(&bar->pv_done[x][hb], (n + 1) & 1));
-        exp32<false, 0>(vb, sl2x2, neg2, lsum, pb, unused);
-        if (!room) {
-          ok = warp_wait<kSuspendNs>(&bar->pv_done[x][hb], (n + 1) & 1, &bar->abort_flag, p.status);
-          if (!ok) break;
+        weights32(vb, sl2x2, neg2, lsum, pb, nullptr, 0);
+        if (n > 0) {                                  // P(u - 2) has been read
+          if (!__all_sync(0xffffffffu, mbar_test(&bar->pv_done[x][hb], (n + 1) & 1))) {
+            ok = warp_wait<kSuspendNs>(&bar->pv_done[x][hb], (n + 1) & 1, &bar->abort_flag, p.status);
+            if (!ok) break;
+          }
+          tc_fence_after();
         }
-        tc_fence_after();
-        tmem_st16(tP, pa);
         tmem_st16(tP + 16, pb);
+        weights32(va, sl2x2, neg2, lsum, pa, lo, (r >> 1) & 3);
+        tmem_st16(tP, pa);
         float a0, a1, b0, b1;
         unpack2(add2(lsum[0], lsum[1]), a0, a1);
         unpack2(add2(lsum[2], lsum[3]), b0, b1);
         l += (a0 + a1) + (b0 + b1);
         // publish P
         tmem_wait_st();
+        if (x == 0) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&bar->p_full[x][hb]);
