@@ -116,7 +116,7 @@ __device__ __forceinline__ void weights32(const uint32_t (&v)[32], uint64_t sl2x
       for (int j = 0; j < 4; ++j) {
         const uint32_t h = pk[4 * c + j];
         float r0, r1;
-        unpack2(add2(pp[j], pack2(-__uint_as_float(h << 16), -__uint_as_float(h & 0xffff0000u))), r0, r1);
+        unpack2(fma2(pack2(__uint_as_float(h << 16), __uint_as_float(h & 0xffff0000u)), pack2(-1.f, -1.f), pp[j]), r0, r1);
         r[j] = pack_bf16(r0, r1);
       }
       *reinterpret_cast<uint4*>(lo + 16 * (c ^ turn)) = make_uint4(r[0], r[1], r[2], r[3]);

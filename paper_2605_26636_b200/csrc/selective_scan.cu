@@ -34,11 +34,17 @@ constexpr int kStagersOf = S == 4 ? 256 : 128;
 constexpr int kTile = 2048;           // tokens times channels of a tile
 constexpr int kStepTokens = 4;        // calls of at most this many tokens walk without tiles
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2eLo = (float)(1.4426950408889634 - (double)1.4426950408889634f);
 
 // log(1 + e^x) = max(x, 0) + log1p(t), t = e^-|x|;  log1p(t) = 2 artanh(t / (2 + t)), the series of artanh up to the 15th power:
 // its argument is 1/3 at most, so what is left out is below 2^-26 of it
 __device__ __forceinline__ float softplus(float x) {
-  const float t = ex2(-fabsf(x) * kLog2e), s = __fdividef(t, 2.f + t), q = s * s;
+  // the exponent's product with log2 e is off by half a unit of its last place, a few 2^-22 of t: what is off is put back; the quotient with
+  // one step of refinement
+  const float e = -fabsf(x), hi = e * kLog2e, lo = fmaf(e, kLog2e, -hi) + e * kLog2eLo;
+  float t = ex2(hi);
+  if (hi > -120.f) t = fmaf(t, lo * 0.69314718f, t);       // (below, and at -inf, there is nothing to put back)
+  const float r = __fdividef(1.f, 2.f + t), s0 = t * r, s = fmaf(fmaf(-s0, 2.f + t, t), r, s0), q = s * s;
   float a = fmaf(q, 1.f / 15.f, 1.f / 13.f);
   a = fmaf(q, a, 1.f / 11.f);
   a = fmaf(q, a, 1.f / 9.f);
