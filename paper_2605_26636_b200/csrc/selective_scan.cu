@@ -1,11 +1,12 @@
 // The selective scan of a state-space mixer: every channel carries Ns states through its sequence.
 //   d_t = softplus(dt_t + dt_bias),  h_t = exp(d_t A) h_(t-1) + d_t B_t u_t,  y_t = (C_t . h_t + D u_t) z_t / (1 + exp(-z_t))
 //
-// Four or eight lanes share a channel, each with a share of its states in registers; a block has 64 or 32 channels in eight warps.  Eight or
-// four more warps bring tiles of 2048 values (32 or 64 tokens) of u, dt, z with their B and C into one of two buffers in shared memory,
-// form d_t and d_t u_t once per token and channel on the way, and take y out of them through D and the gate.  (Bringing tiles in between steps of the eight
-// warps themselves left both kinds of work waiting: two prompts of 4096 tokens, 2048 channels, 16 states 231 us.)  As many tokens at a time as a channel has lanes: the lanes' shares
-// of their y are exchanged so that every lane ends up with the sum of one.  States in pairs (the packed fp32 arithmetic of sm_100).
+// Four or eight lanes share a channel, each with a share of its states in registers; a block has 64 or 32 channels in eight warps.
+// Eight more warps bring tiles of 2048 values (32 or 64 tokens) of u, dt, z with their B and C into one of two buffers in shared
+// memory, form d_t and d_t u_t once per token and channel on the way, and take y out of them through D and the gate.  (Bringing
+// tiles in between steps of the computing warps themselves left both kinds of work waiting: two prompts of 4096 tokens, 2048
+// channels, 16 states 231 us against 183.)  As many tokens at a time as a channel has lanes: the lanes' shares of their y are
+// exchanged so that every lane ends up with the sum of one.  States in pairs (the packed fp32 arithmetic of sm_100).
 //
 // What bounds it: the exponentials, Ns a token and channel on the MUFU unit (16 a clock and SM), more than twice what
 // the bytes take at Ns = 16 in bf16.
@@ -27,10 +28,9 @@ using tc::pack2;
 using tc::unpack2;
 
 constexpr int kThreads = 256;         // that compute
-// ... and that bring tiles in and out.  Four lanes a channel: two blocks an SM, 512 threads each.  Measured with 256 / 128 of them, B x L tokens of
-// 2048 channels: 4 x 2048 163 / 234 us, 8 x 2048 278 / 315; eight lanes, one block an SM: 2 x 4096 184 / 180.
-template <int S>
-constexpr int kStagersOf = S == 4 ? 256 : 128;
+// ... and that bring tiles in and out.  Measured with 256 / 128 of them, B x L tokens of 2048 channels: 2 x 4096 183 / 220 us, 4 x 2048 163 / 234,
+// 8 x 2048 286 / 315.
+constexpr int kStagers = 256;
 constexpr int kTile = 2048;           // tokens times channels of a tile
 constexpr int kStepTokens = 4;        // calls of at most this many tokens walk without tiles
 constexpr float kLog2e = 1.4426950408889634f;
@@ -180,16 +180,14 @@ struct Smem {
 
 // Barriers of a block: a buffer is full (it waits for the warps that bring tiles in); a buffer is done with (they wait for the others)
 constexpr int kFull = 1, kDone = 3;
-template <int S>
-__device__ __forceinline__ void barrier_sync(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kThreads + kStagersOf<S>) : "memory"); }
-template <int S>
-__device__ __forceinline__ void barrier_arrive(int id) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(kThreads + kStagersOf<S>) : "memory"); }
+__device__ __forceinline__ void barrier_sync(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kThreads + kStagers) : "memory"); }
+__device__ __forceinline__ void barrier_arrive(int id) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(kThreads + kStagers) : "memory"); }
 
 // The warps that bring tiles in, two ahead of the others, and y out
 template <typename T, int S, int NPL, bool WIDE, bool kY>
 __device__ __forceinline__ void stage_tiles(const ScanArgs& a, Smem<T, S, NPL>* buf, int b, int c0, int t_begin, int t_end, int tiles) {
   using Sm = Smem<T, S, NPL>;
-  constexpr int kCh = Sm::kCh, kTT = Sm::kTT, kStagers = kStagersOf<S>;
+  constexpr int kCh = Sm::kCh, kTT = Sm::kTT;
   constexpr int kVec = WIDE ? 16 / sizeof(T) : 1;             // elements of a load
   constexpr int kLoads = kTile / kStagers / kVec;             // loads of a thread and tile from each of u, dt, z
   constexpr int kRow = kCh / kVec;                            // loads of a token
@@ -308,23 +306,23 @@ __device__ __forceinline__ void stage_tiles(const ScanArgs& a, Smem<T, S, NPL>* 
   for (int i = 0; i < min(2, tiles); ++i) {
     fetch(t_begin + i * kTT);
     put(buf[i], t_begin + i * kTT);
-    barrier_arrive<S>(kFull + i);
+    barrier_arrive(kFull + i);
   }
   for (int i = 0; i < tiles; ++i) {
     const int t0 = t_begin + i * kTT;
     if (i + 2 < tiles) fetch(t0 + 2 * kTT);
-    barrier_sync<S>(kDone + (i & 1));
+    barrier_sync(kDone + (i & 1));
     if (kY) flush(buf[i & 1], t0);                              // (a thread reads and refills the same places of u)
     if (i + 2 < tiles) {
       put(buf[i & 1], t0 + 2 * kTT);
-      barrier_arrive<S>(kFull + (i & 1));
+      barrier_arrive(kFull + (i & 1));
     }
   }
 }
 
 // S lanes a channel, NPL states a lane.  kY: the whole thing; else the chunk's own state from zero and the sum of its steps only
 template <typename T, int S, int NPL, bool WIDE, bool kY>
-__global__ void __launch_bounds__(kThreads + kStagersOf<S>, S == 4 && NPL <= 4 ? 2 : 1) scan_kernel(const ScanArgs a, int chunk, int nchunk, float* ws_state, float* ws_sum) {
+__global__ void __launch_bounds__(kThreads + kStagers, S == 4 && NPL <= 4 ? 2 : 1) scan_kernel(const ScanArgs a, int chunk, int nchunk, float* ws_state, float* ws_sum) {
   using Sm = Smem<T, S, NPL>;
   constexpr int kCh = Sm::kCh, kTT = Sm::kTT;
   extern __shared__ __align__(16) unsigned char smem_raw[];
@@ -355,7 +353,7 @@ __global__ void __launch_bounds__(kThreads + kStagersOf<S>, S == 4 && NPL <= 4 ?
   for (int i = 0; i < tiles; ++i) {
     Sm& sm = buf[i & 1];
     const int t0 = t_begin + i * kTT;
-    barrier_sync<S>(kFull + (i & 1));
+    barrier_sync(kFull + (i & 1));
     const int tokens = min(kTT, t_end - t0);
 #pragma unroll 1
     for (int t = 0; t < tokens; t += S) {                       // (kTT is a multiple of S; tokens past the end change nothing)
@@ -422,7 +420,7 @@ __global__ void __launch_bounds__(kThreads + kStagersOf<S>, S == 4 && NPL <= 4 ?
         sm.y[t + s][lc] = y[0];
       }
     }
-    barrier_arrive<S>(kDone + (i & 1));
+    barrier_arrive(kDone + (i & 1));
   }
   if (c >= a.C) return;
 #pragma unroll
@@ -468,13 +466,13 @@ cudaError_t launch_tiles(const ScanArgs& a, const ScanPlan& p, void* ws, cudaStr
   float* state = p.nchunk > 1 ? (float*)((char*)ws + p.off_state) : nullptr;
   float* sum = p.nchunk > 1 ? (float*)((char*)ws + p.off_sum) : nullptr;
   if (p.nchunk > 1) {
-    e = launch_programmatic(scan_kernel<T, S, NPL, WIDE, false>, grid, kThreads + kStagersOf<S>, 2 * sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
+    e = launch_programmatic(scan_kernel<T, S, NPL, WIDE, false>, grid, kThreads + kStagers, 2 * sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
     if (e != cudaSuccess) return e;
     const int64_t n = (int64_t)a.B * a.C * a.Ns;
     e = launch_programmatic(scan_carry_kernel, dim3((unsigned)((n + 255) / 256)), 256, 0, st, a, p.nchunk, state, (const float*)sum);
     if (e != cudaSuccess) return e;
   }
-  return launch_programmatic(scan_kernel<T, S, NPL, WIDE, true>, grid, kThreads + kStagersOf<S>, 2 * sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
+  return launch_programmatic(scan_kernel<T, S, NPL, WIDE, true>, grid, kThreads + kStagers, 2 * sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
 }
 
 template <typename T, int S, int NPL>
