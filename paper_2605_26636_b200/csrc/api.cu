@@ -145,7 +145,8 @@ jv_status check_norm(const jv_norm_shape* s) {
   if (s->dtype != JV_F32 && s->dtype != JV_BF16) return JV_ERR_INVALID_ARG;
   if (s->C > 16384 || s->rows > 0x7fffffffll) return JV_ERR_UNSUPPORTED;
   if ((s->x_stride != 0 && s->x_stride < s->C) || (s->dy_stride != 0 && s->dy_stride < s->C)) return JV_ERR_INVALID_ARG;
-  if (s->x_stride > ((int64_t)1 << 31) || s->dy_stride > ((int64_t)1 << 31)) return JV_ERR_UNSUPPORTED;
+  for (int64_t stride : {s->x_stride, s->dy_stride})          // (extents are counted in 64 bits of bytes)
+    if (stride > ((int64_t)1 << 56) / s->rows) return JV_ERR_UNSUPPORTED;
   return JV_OK;
 }
 size_t norm_rows_bytes(const jv_norm_shape* s, int64_t stride) {
@@ -158,7 +159,8 @@ bool token_rows(const int64_t* s, int L, int C, Rows* out) {
   out->batch = s[1] ? s[1] : L * out->tok;
   return out->tok >= C && out->batch > 0;
 }
-bool far_rows(const Rows& r) { return r.tok > (int64_t)1 << 31 || r.batch > (int64_t)1 << 55; }
+// extents are counted in 64 bits of bytes (L is at most 2^24)
+bool far_rows(const Rows& r, int B) { return r.tok > (int64_t)1 << 31 || r.batch > ((int64_t)1 << 56) / B; }
 
 // {tokens, heads, batch elements}; a zero entry only where all are zero (contiguous)
 bool diff_strides(const int64_t* s, int heads, int n, int D, InStrides* out) {
@@ -193,7 +195,7 @@ jv_status check_conv(const jv_conv_shape* s, Rows* xs) {
   if (!s || s->B <= 0 || s->L <= 0 || s->C <= 0 || s->K <= 0) return JV_ERR_INVALID_ARG;
   if (s->dtype != JV_F32 && s->dtype != JV_BF16) return JV_ERR_INVALID_ARG;
   if ((s->silu != 0 && s->silu != 1) || !token_rows(s->x_stride, s->L, s->C, xs)) return JV_ERR_INVALID_ARG;
-  if (s->K < 2 || s->K > 4 || s->B > 65535 || s->C > (1 << 20) || s->L > (1 << 24) || far_rows(*xs)) return JV_ERR_UNSUPPORTED;
+  if (s->K < 2 || s->K > 4 || s->B > 65535 || s->C > (1 << 20) || s->L > (1 << 24) || far_rows(*xs, s->B)) return JV_ERR_UNSUPPORTED;
   return (int64_t)s->B * s->L * s->C > ((int64_t)1 << 40) ? JV_ERR_UNSUPPORTED : JV_OK;
 }
 
@@ -208,7 +210,7 @@ jv_status check_scan(const jv_scan_shape* s, ScanRows* r) {
       !token_rows(s->b_stride, s->L, s->Ns, &r->b) || !token_rows(s->c_stride, s->L, s->Ns, &r->c))
     return JV_ERR_INVALID_ARG;
   for (const Rows& v : {r->u, r->dt, r->b, r->c, r->z})
-    if (far_rows(v)) return JV_ERR_UNSUPPORTED;
+    if (far_rows(v, s->B)) return JV_ERR_UNSUPPORTED;
   if (s->Ns > 64 || s->B > 65535 || s->C > (1 << 20) || s->L > (1 << 24)) return JV_ERR_UNSUPPORTED;
   return JV_OK;
 }
@@ -525,7 +527,7 @@ size_t jv_diff_attn_workspace_bytes(const jv_diff_shape* shape) {
   if (check_diff(shape, &qs, &ks) != JV_OK) return 0;
   if (shape->dtype != JV_BF16 || shape->D != 64) return 0;                // (the fp32 kernel needs none)
   const int pairs = shape->H / 2, kv_pairs = shape->Hkv / 2;
-  const size_t tiles = diff_tc_plan(shape->B, pairs, shape->Nq, shape->Nk, shape->causal != 0).total;
+  const size_t tiles = diff_tc_plan(shape->B, pairs, shape->Nq, shape->Nk).total;
   const size_t rows = diff_rows_plan(shape->B, kv_pairs, shape->Nk).total;
   return (int64_t)(pairs / kv_pairs) * shape->Nq <= 16 ? rows : tiles;
 }

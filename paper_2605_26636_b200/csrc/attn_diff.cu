@@ -536,8 +536,7 @@ constexpr int kTilesMin = 4;
 // An item costs as much as four tiles beside its own (first scores, epilogue).  Measured, in units of 1 / 2 / 3 / 4 / 6 tiles: two
 // causal prompts of 4096 tokens, 8 pairs, 176 / 143 / 125 / 124 / 128 us, with none 231; 73 x 73 tokens 658 to 664, 6: 694.
 constexpr int kLead = 4, kWhole = 2;
-int diff_blocks(int B, int pairs, int Nq, int Nk, bool causal) {
-  (void)causal;
+int diff_blocks(int B, int pairs, int Nq, int Nk) {
   const int64_t items = (int64_t)B * pairs * ceil_div(Nq, kTile), tiles = items * ceil_div(Nk, kTile);
   const int64_t want = items > tiles / kTilesMin ? items : tiles / kTilesMin;
   const int sms = device_sm_count();
@@ -546,8 +545,8 @@ int diff_blocks(int B, int pairs, int Nq, int Nk, bool causal) {
 
 }  // namespace
 
-DiffPlan diff_tc_plan(int B, int pairs, int Nq, int Nk, bool causal) {
-  return diff_plan(diff_blocks(B, pairs, Nq, Nk, causal), kTile, (int64_t)B * pairs * Nq);
+DiffPlan diff_tc_plan(int B, int pairs, int Nq, int Nk) {
+  return diff_plan(diff_blocks(B, pairs, Nq, Nk), kTile, (int64_t)B * pairs * Nq);
 }
 
 bool diff_tc_supported(const DiffArgs& a) { return a.dtype == JV_BF16 && a.D == kD && encode_fn() != nullptr; }
@@ -574,7 +573,7 @@ cudaError_t launch_diff_tc(const DiffArgs& a, void* ws, int* status, cudaStream_
     return cudaFuncSetAttribute(attn_diff_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes);
   });
   if (e != cudaSuccess) return e;
-  const DiffPlan plan = diff_tc_plan(a.B, a.pairs, a.Nq, a.Nk, a.causal);
+  const DiffPlan plan = diff_tc_plan(a.B, a.pairs, a.Nq, a.Nk);
   const DiffParams p = diff_params(a, plan, Items{a.B, ceil_div(a.Nq, kTile), a.pairs, a.Nq, a.Nk, kTile, a.causal ? 1 : 0, kLead, kWhole, a.kv_len, a.q_pos},
                                    kTile, ws, status);
   e = launch_programmatic(attn_diff_kernel, dim3((unsigned)plan.blocks), kThreads, kSmemBytes, st, maps[0], maps[1], maps[2], p);

@@ -45,7 +45,8 @@ struct Reach {
 __device__ __forceinline__ Reach reach_of(const int* kv_len, const int* q_pos, int b, int Nq, int Nk, bool causal) {
   Reach r;
   r.len = kv_len ? min(max(__ldg(kv_len + b), 0), Nk) : Nk;
-  r.pos = q_pos ? min(__ldg(q_pos + b), Nk) : Nk - Nq;       // (a position past the last key sees them all)
+  // a position past the last key sees them all, one that the last query does not bring up to key 0 sees none, however far off it is
+  r.pos = q_pos ? max(min(__ldg(q_pos + b), Nk), -Nq) : Nk - Nq;
   r.causal = causal;
   return r;
 }
@@ -343,7 +344,7 @@ DiffPlan diff_rows_plan(int B, int kv_pairs, int Nk);
 cudaError_t launch_diff_rows(const DiffArgs& a, void* ws, int* status, cudaStream_t st);
 // ... or tiles of 128 queries of a pair
 bool diff_tc_supported(const DiffArgs& a);
-DiffPlan diff_tc_plan(int B, int pairs, int Nq, int Nk, bool causal);
+DiffPlan diff_tc_plan(int B, int pairs, int Nq, int Nk);
 cudaError_t launch_diff_tc(const DiffArgs& a, void* ws, int* status, cudaStream_t st);
 
 }  // namespace jv

@@ -59,6 +59,12 @@ __device__ __forceinline__ float silu(float x) { return __fdividef(x, 1.f + ex2(
 
 __device__ __forceinline__ int length_of(const ScanArgs& a, int b) { return a.lens ? min(max(__ldg(a.lens + b), 0), a.L) : a.L; }
 
+// A coefficient, for powers of 2.  Minus infinity (a state that is forgotten at once) as the lowest number: a step of 0, as tokens and chunks
+// past the end have it, then leaves the state alone, as it does elsewhere.
+__device__ __forceinline__ float coefficient(float A) {
+  const float a = A * kLog2e;
+  return a < -3.4028235e38f ? -3.4028235e38f : a;
+}
 // A channel's coefficients and states: state n of lane s is s * NPL + n; states past Ns are zeros all through
 template <int NPL>
 __device__ __forceinline__ void load_A(const ScanArgs& a, int c, int s, float (&A2)[NPL]) {
@@ -66,12 +72,12 @@ __device__ __forceinline__ void load_A(const ScanArgs& a, int c, int s, float (&
 #pragma unroll
     for (int n = 0; n + 3 < NPL; n += 4) {
       const float4 v = s * NPL + n < a.Ns ? __ldg(reinterpret_cast<const float4*>(a.A + (int64_t)c * a.Ns + s * NPL + n)) : make_float4(0.f, 0.f, 0.f, 0.f);
-      A2[n] = v.x * kLog2e; A2[n + 1] = v.y * kLog2e; A2[n + 2] = v.z * kLog2e; A2[n + 3] = v.w * kLog2e;
+      A2[n] = coefficient(v.x); A2[n + 1] = coefficient(v.y); A2[n + 2] = coefficient(v.z); A2[n + 3] = coefficient(v.w);
     }
     return;
   }
 #pragma unroll
-  for (int n = 0; n < NPL; ++n) A2[n] = s * NPL + n < a.Ns ? __ldg(a.A + (int64_t)c * a.Ns + s * NPL + n) * kLog2e : 0.f;
+  for (int n = 0; n < NPL; ++n) A2[n] = s * NPL + n < a.Ns ? coefficient(__ldg(a.A + (int64_t)c * a.Ns + s * NPL + n)) : 0.f;
 }
 template <int NPL>
 __device__ __forceinline__ void load_state(const float* h, int Ns, int s, float (&st)[NPL]) {
@@ -443,7 +449,7 @@ __global__ void __launch_bounds__(256) scan_carry_kernel(const ScanArgs a, int n
   if (b >= a.B) return;
   const int64_t e = id - b * per;
   const int c = (int)(e / a.Ns);
-  const float A2 = __ldg(a.A + e) * kLog2e;
+  const float A2 = coefficient(__ldg(a.A + e));
   float h = a.h_in ? a.h_in[b * per + e] : 0.f;
   for (int k = 0; k < nchunk; ++k) {
     float* st = ws_state + ((int64_t)b * nchunk + k) * per + e;

@@ -467,13 +467,17 @@ def _enqueue(dev: int, stream, call):
         return call(_stream(stream))
 
 
+def _new(shape, dtype, device, stream) -> torch.Tensor:
+    """A tensor that the call writes, from the memory of the stream that it runs on: what is free there, no earlier work of
+    another stream still uses."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _scratch(n: int, device, stream) -> Optional[torch.Tensor]:
-    if n == 0:
-        return None
-    ws = torch.empty(n, dtype=torch.uint8, device=device)
-    if stream is not None:
-        ws.record_stream(stream)          # freed by torch on the current stream, used on `stream`
-    return ws
+    return _new(n, torch.uint8, device, stream) if n else None
 
 
 def _rows(t: torch.Tensor, what: str):
@@ -508,7 +512,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-6, out=None, stats=Non
         _per_row(mean, rows, _F32, dev, "stats")
         _per_row(rstd, rows, _F32, dev, "stats")
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _new(x.shape, x.dtype, x.device, stream)
     else:
         _like(out, x.shape, x.dtype, dev, "out")
     shape = JvNormShape(rows, C, _dtype_code(x), stride)
@@ -531,8 +535,8 @@ def layer_norm_grad(dy, x, weight, mean, rstd, weight_grad: bool = True, bias_gr
     _per_row(mean, rows, _F32, dev, "mean")
     _per_row(rstd, rows, _F32, dev, "rstd")
     if out is None:
-        new = lambda want: torch.empty(C, dtype=_F32, device=x.device) if want else None
-        dx, dw, db = out = (torch.empty(x.shape, dtype=x.dtype, device=x.device), new(weight_grad), new(bias_grad))
+        new = lambda want: _new(C, _F32, x.device, stream) if want else None
+        dx, dw, db = out = (_new(x.shape, x.dtype, x.device, stream), new(weight_grad), new(bias_grad))
     else:
         dx, dw, db = out
         _like(dx, x.shape, x.dtype, dev, "dx")
@@ -594,7 +598,7 @@ def diff_attn(q, k, v, lam, lambda_init: float, norm_weight=None, norm_eps: floa
         _per_row(q_pos, B, _I32, dev, "q_pos")
     d = JvDiff(lam.data_ptr(), lambda_init, _ptr(norm_weight), norm_eps, _ptr(kv_len), _ptr(q_pos))
     if out is None:
-        out = torch.empty(qs, dtype=dtype, device=q.device)
+        out = _new(qs, dtype, q.device, stream)
     else:
         _like(out, qs, dtype, dev, "out")
 
@@ -645,7 +649,7 @@ def causal_conv(x, weight, bias=None, state=None, state_out=None, lens=None, sil
     if lens is not None:
         _per_row(lens, B, _I32, dev, "lens")
     if out is None:
-        out = torch.empty(xs, dtype=dtype, device=x.device)
+        out = _new(xs, dtype, x.device, stream)
     else:
         _like(out, xs, dtype, dev, "out")
     st = _enqueue(dev, stream, lambda s: lib().jv_causal_conv(
@@ -680,7 +684,7 @@ def selective_scan(u, dt, A, Bm, Cm, D=None, z=None, dt_bias=None, state=None, s
     if lens is not None:
         _per_row(lens, B, _I32, dev, "lens")
     if out is None:
-        out = torch.empty(us, dtype=dtype, device=u.device)
+        out = _new(us, dtype, u.device, stream)
     else:
         _like(out, us, dtype, dev, "out")
 

@@ -123,6 +123,33 @@ def test_lengths_positions_and_garbage_behind_them(Nq, Nk, causal):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("Nq,Nk,dtype", [(1, 700, torch.bfloat16), (200, 700, torch.bfloat16), (5, 90, torch.float32)])
+def test_positions_at_the_ends_of_their_type(Nq, Nk, dtype):
+    q, k, v, lam, w = _tensors(5, 4, 2, Nq, Nk, dtype=dtype)
+    pos = torch.tensor([-1 << 31, (1 << 31) - 1, (-1 << 31) + 70, -Nq, (1 << 31) - Nq], dtype=torch.int32, device="cuda")
+    o = _check(q, k, v, lam, w, causal=True, q_pos=pos, rms=False)
+    assert (o[0] == 0).all() and (o[2] == 0).all() and (o[3] == 0).all() and (o[1] != 0).any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("Nq,Nk", [(1, 2000), (256, 500)])
+def test_results_on_another_stream_do_not_lie_where_earlier_work_still_writes(Nq, Nk):
+    q, k, v, lam, w = _tensors(2, 8, 4, Nq, Nk)
+    want = jv.diff_attn(q, k, v, lam, 0.8, norm_weight=w)
+    shape = _shape(2, 8, 4, Nq, Nk)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    late = [torch.empty_like(q), torch.empty(jv.lib().jv_diff_attn_workspace_bytes(ctypes.byref(shape)), dtype=torch.uint8, device="cuda")]
+    torch.cuda._sleep(1 << 26)
+    for t in late:
+        t.fill_(7)
+    del late, t
+    got = jv.diff_attn(q, k, v, lam, 0.8, norm_weight=w, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("Nq,Nk", [(1, 900), (260, 260)])
 def test_layouts(Nq, Nk):
     q, k, v, lam, w = _tensors(2, 4, 4, Nq, Nk)

@@ -204,6 +204,26 @@ def test_captured_and_on_another_stream():
 X, W, Y, M, R, DY, WS = (i << 24 for i in range(1, 8))
 
 
+@pytest.mark.gpu
+def test_results_on_another_stream_do_not_lie_where_earlier_work_still_writes():
+    """Memory that this stream has freed may have work ahead of it here; a call for another stream takes none of it."""
+    x, dy, w, b = _inputs(4096, 512, torch.float32)
+    stats = torch.empty(4096, device="cuda"), torch.empty(4096, device="cuda")
+    want = jv.layer_norm(x, w, b, stats=stats)
+    want_g = jv.layer_norm_grad(dy, x, w, *stats)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    late = [torch.empty_like(x) for _ in range(2)] + [torch.empty(512, device="cuda") for _ in range(2)]
+    late.append(torch.empty(int(jv.lib().jv_layer_norm_grad_workspace_bytes(ctypes.byref(jv.JvNormShape(4096, 512, jv.JV_F32, 0, 0)))), dtype=torch.uint8, device="cuda"))
+    torch.cuda._sleep(1 << 26)
+    for t in late:
+        t.fill_(7)
+    del late, t
+    got, got_g = jv.layer_norm(x, w, b, stream=side), jv.layer_norm_grad(dy, x, w, *stats, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and all(torch.equal(a, e) for a, e in zip(got_g, want_g))
+
+
 @pytest.fixture(scope="module")
 def L():
     jv_build.build()
@@ -223,6 +243,8 @@ def test_refusals(L):
         assert _fwd(L, **kw) == bad, kw
     assert _fwd(L, shp=S(8, 16385, 0, 0, 0)) == jv.JV_ERR_UNSUPPORTED
     assert _fwd(L, shp=S(1 << 31, 64, 0, 0, 0)) == jv.JV_ERR_UNSUPPORTED
+    for strides in ((1 << 31, 0), (0, 1 << 31)):                     # extents that 64 bits of bytes do not hold
+        assert _fwd(L, shp=S((1 << 31) - 1, 64, 0, *strides)) == jv.JV_ERR_UNSUPPORTED
     shp = S(8, 64, jv.JV_F32, 0, 0)
     need = L.jv_layer_norm_grad_workspace_bytes(ctypes.byref(shp))
     assert need >= 2 * 64 * 4 and L.jv_layer_norm_grad_workspace_bytes(ctypes.byref(S(0, 64, 0, 0, 0))) == 0

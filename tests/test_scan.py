@@ -224,6 +224,42 @@ def test_far_values_and_no_numbers():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("B,L,C,Ns", [(2, 1, 100, 16), (2, 37, 5000, 16), (3, 1000, 64, 16), (2, 600, 100, 33)])
+def test_states_that_are_forgotten_at_once(B, L, C, Ns, dtype):
+    """A of minus infinity: what any A gives that forgets within a step; tokens and chunks past the end leave the state alone."""
+    i = _scan_inputs(B, L, C, Ns, dtype)
+    lens = torch.tensor([max(1, L - 401 * b) for b in range(B)], dtype=torch.int32, device="cuda")
+    i["A"][:, 1::3] = -1e30
+    _scan_check(i, dtype, lens)
+    at_once = dict(i, A=torch.where(i["A"] == -1e30, -math.inf, i["A"]))
+    h, hw = (torch.empty_like(i["state"]) for _ in range(2))
+    out, want = (torch.zeros(B, L, C, dtype=dtype, device="cuda") for _ in range(2))
+    jv.selective_scan(**at_once, lens=lens, out=out, state_out=h)
+    jv.selective_scan(**i, lens=lens, out=want, state_out=hw)
+    assert torch.equal(out, want) and torch.equal(h, hw) and torch.isfinite(h).all()
+
+
+@pytest.mark.gpu
+def test_results_on_another_stream_do_not_lie_where_earlier_work_still_writes():
+    i = _scan_inputs(1, 1000, 256, 16, torch.float32)
+    w = torch.randn(256, 4, device="cuda")
+    want, want_c = jv.selective_scan(**i), jv.causal_conv(i["u"], w)
+    shape = jv.JvScanShape(1, 1000, 256, 16, jv.JV_F32, 1)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    late = [torch.empty_like(want), torch.empty_like(want),
+            torch.empty(jv.lib().jv_selective_scan_workspace_bytes(ctypes.byref(shape)), dtype=torch.uint8, device="cuda")]
+    torch.cuda._sleep(1 << 26)
+    for t in late:
+        t.fill_(7)
+    del late, t
+    got, got_c = jv.selective_scan(**i, stream=side), jv.causal_conv(i["u"], w, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(got_c, want_c)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("B,L,C", [(2, 1, 300), (1, 700, 192)])
 def test_streams_and_capture(B, L, C):
     i = _scan_inputs(B, L, C, 16, torch.bfloat16)
@@ -273,6 +309,8 @@ def test_conv_refusals(L):
         assert call(**kw) == jv.JV_ERR_INVALID_ARG, kw
     for shp in (S(2, 8, 64, 1, 0, 1), S(2, 8, 64, 5, 0, 1), S(70000, 8, 64, 4, 0, 1)):
         assert call(shp=shp) == jv.JV_ERR_UNSUPPORTED
+    far = S(65535, 8, 64, 4, 0, 1, (64, 1 << 55))                      # extents that 64 bits of bytes do not hold
+    assert call(shp=far) == jv.JV_ERR_UNSUPPORTED
     if not torch.cuda.is_available():
         assert call() in (jv.JV_ERR_CUDA, jv.JV_ERR_UNSUPPORTED)
     t = torch.zeros(1, 4, 8)
@@ -298,6 +336,7 @@ def test_scan_refusals(L):
     for kw in bad:
         assert call(**kw) == jv.JV_ERR_INVALID_ARG, kw
     assert call(shp=S(2, 8, 64, 65, 0, 1)) == jv.JV_ERR_UNSUPPORTED
+    assert call(shp=S(65535, 8, 64, 16, 0, 1, (64, 1 << 55))) == jv.JV_ERR_UNSUPPORTED
     for kw in (dict(ws=None), dict(ws=P[12] + 8), dict(n=need - 1)):
         assert call(**kw) == jv.JV_ERR_WORKSPACE, kw
     one = S(2, 1, 64, 16, jv.JV_F32, 1)
