@@ -444,21 +444,21 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
       if (!it.whole()) {
         // ---- a part: reference, sum and product of this map as they are, half the channels to each set.  Reference -inf: no
         // keys of this row; none at all: the row has to be done again.
-        float* dst = p.partial + ((size_t)partial_slot(blockIdx.x, it.t0) * kTile + r) * kPartial;
+        float* dst = p.partial + partial_at((size_t)partial_slot(blockIdx.x, it.t0) * kTile + r);
         if (hb == 0) {
           const float s = bar->sum[x][0][r] + bar->sum[x][1][r];
           const float ref = limit <= it.t0 * kTile ? -INFINITY : fine(s) ? -bar->ref[x][r] : __uint_as_float(0x7fc00000u);
           *reinterpret_cast<float2*>(dst + 2 * x) = make_float2(ref, s);
         }
-        dst += 4 + kV * x + kD * hb;
-#pragma unroll 1
+        dst += (1 + (kV * x + kD * hb) / 4) * kPiece;
+#pragma unroll
         for (int c = 0; c < kD / 32; ++c) {
           uint32_t v[32];
           tmem_ld32(tO + kV * x + kD * hb + 32 * c, v);
           tmem_wait_ld(v);
 #pragma unroll
           for (int y = 0; y < 8; ++y)
-            *reinterpret_cast<uint4*>(dst + 32 * c + 4 * y) = make_uint4(v[4 * y], v[4 * y + 1], v[4 * y + 2], v[4 * y + 3]);
+            *reinterpret_cast<uint4*>(dst + (8 * c + y) * kPiece) = make_uint4(v[4 * y], v[4 * y + 1], v[4 * y + 2], v[4 * y + 3]);
         }
         tc_fence_before();
         mbar_arrive(&bar->read_out);

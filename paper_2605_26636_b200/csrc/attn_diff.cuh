@@ -34,7 +34,12 @@ namespace diff {
 
 constexpr int kD = 64, kV = 128;     // channels of a map; of a value row
 constexpr int kTile = 128;           // keys of a tile
-constexpr int kPartial = 4 + 2 * kV; // floats of a row's partial: reference (log2) and sum of map 0, of map 1, product 0, product 1
+// A row's partial: 65 pieces of 16 bytes, reference (log2) and sum of map 0 and of map 1, product 0, product 1.  The pieces of sixteen rows
+// lie side by side, [16 rows / piece / row]: threads that own rows write, and threads that own channels of sixteen rows read, 256
+// bytes in a row.  (Row by row the main launch's stores, 16 bytes of 32 rows at a time, took a quarter of 256 queries against
+// 16384 keys.)
+constexpr int kPartial = 4 + 2 * kV, kPartialRows = 16, kPiece = 4 * kPartialRows;   // floats of a row; rows side by side; floats from piece to piece
+__host__ __device__ constexpr size_t partial_at(size_t row) { return row / kPartialRows * (kPartialRows * kPartial) + row % kPartialRows * 4; }
 
 // Keys that a batch element has, and the position of its first query among them.  A query i sees the keys [0, limit(i)).
 struct Reach {

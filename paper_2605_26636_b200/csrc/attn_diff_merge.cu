@@ -9,12 +9,13 @@ namespace {
 using namespace tc;
 using namespace diff;
 
-// Block (c, y): the marked rows of the whole items of block c of the main launch; and the item that block c takes up in its middle, if c
-// is the first that does.  Sixteen lanes a row, eight channels of both maps each: two rows to a warp, sixteen to a block.
+// Block (c, y): the marked rows of the whole items of block c of the main launch; and sixteen rows, 16 y on, of the item that block c
+// takes up in its middle, if c is the first that does.  A thread has eight channels of both maps of one row.
 constexpr int kMergeWarps = 8;
-constexpr int kMergeRows = 2 * kMergeWarps;
+constexpr int kMergeRows = 16;
+static_assert(kMergeRows == kPartialRows && kMergeWarps * 32 == kMergeRows * kV / 8, "threads of the rows that lie side by side");
 __global__ void __launch_bounds__(kMergeWarps * 32, 4) diff_merge_kernel(const DiffParams p, int rows, int blocks) {
-  __shared__ float sq[kMergeWarps][kV];
+  __shared__ float sq[kMergeWarps][kV], square[kMergeWarps][kMergeRows];
   griddep_wait();
   griddep_launch_dependents();
   const int c = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -56,73 +57,75 @@ __global__ void __launch_bounds__(kMergeWarps * 32, 4) diff_merge_kernel(const D
   }
   if (left) return;                          // blocks that have left without a result
   const Reach reach = reach_of(p.items.kv_len, p.items.q_pos, s.b, p.items.Nq, p.items.Nk, p.items.causal != 0);
-  const int sub = lane >> 4, ch = 8 * (lane & 15);
-  for (int r0 = blockIdx.y * kMergeRows + 2 * warp; r0 < rows; r0 += gridDim.y * kMergeRows) {
-    const int r = min(r0 + sub, rows - 1);
-    int pair, i;
-    p.row(s.qt, s.pair, r, pair, i);
-    const bool mine = r0 + sub < rows && i < p.items.Nq;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, acc[2][8];
+  const int row = lane & 15, r = kMergeRows * blockIdx.y + row, ch = 8 * (2 * warp + (lane >> 4));
+  int pair, i;
+  p.row(s.qt, s.pair, min(r, rows - 1), pair, i);
+  const bool mine = r < rows && i < p.items.Nq;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, acc[2][8];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+  for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int y = 0; y < 8; ++y) acc[h][y] = 0.f;
-    const float* src = p.partial + r * kPartial;
+    for (int y = 0; y < 8; ++y) acc[h][y] = 0.f;
+  const float* src = p.partial + partial_at(r);
 #pragma unroll 2
-    for (int k = begun; k <= last; ++k) {
-      // (a block without tiles has left nothing in its slots: what lies there is loaded and dropped)
-      const float* at = src + (size_t)(2 * k + (k == begun ? 1 : 0)) * p.slot_rows * kPartial;
-      const float4 st = __ldcg(reinterpret_cast<const float4*>(at));
-      float4 q[2][2];
+  for (int k = begun; k <= (mine ? last : -1); ++k) {
+    // (a block without tiles has left nothing in its slots: what lies there is loaded and dropped)
+    const float* at = src + (size_t)(2 * k + (k == begun ? 1 : 0)) * p.slot_rows * kPartial;
+    const float4 st = __ldcg(reinterpret_cast<const float4*>(at));
+    float4 q[2][2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int y = 0; y < 2; ++y) q[h][y] = __ldcg(reinterpret_cast<const float4*>(at + 4 + kV * h + ch + 4 * y));
-      const bool none = k > begun && p.starts[k].tiles == 0;
-      const float pm[2] = {st.x, st.z}, pl[2] = {st.y, st.w};
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (none || pm[h] == -INFINITY) continue;       // no keys of this row
-        const float mn = max3(m[h], pm[h], pm[h]), f = ex2(m[h] - mn), g = ex2(pm[h] - mn);
-        m[h] = mn;
-        l[h] = l[h] * f + pl[h] * g;
-        const float v[8] = {q[h][0].x, q[h][0].y, q[h][0].z, q[h][0].w, q[h][1].x, q[h][1].y, q[h][1].z, q[h][1].w};
-#pragma unroll
-        for (int y = 0; y < 8; ++y) acc[h][y] = acc[h][y] * f + v[y] * g;
-      }
-    }
-    const bool any = reach.limit(i) > 0;
-    const float f0 = any ? 1.f / l[0] : 0.f, f1 = any ? -lam / l[1] : 0.f;
-    float x[8], ss = 0.f;
-#pragma unroll
-    for (int y = 0; y < 8; ++y) {
-      x[y] = acc[0][y] * f0 + acc[1][y] * f1;
-      ss = fmaf(x[y], x[y], ss);
-    }
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    const bool again = mine && !(ss < INFINITY);   // a part that says so, or values out of range
-    if (p.tail.norm_w) {
-      const float rn = (1.f - p.tail.lambda_init) * rsqrtf(ss * (1.f / kV) + p.tail.norm_eps);
-#pragma unroll
-      for (int y = 0; y < 8; y += 4) {
-        const float4 w = __ldg(reinterpret_cast<const float4*>(p.tail.norm_w + ch + y));
-        x[y] *= rn * w.x; x[y + 1] *= rn * w.y; x[y + 2] *= rn * w.z; x[y + 3] *= rn * w.w;
-      }
-    }
-    if (mine && !again) {
-      __nv_bfloat16* dst = p.o + (((size_t)s.b * 2 * p.pairs + 2 * pair + (ch >> 6)) * p.items.Nq + i) * kD + (ch & 63);
-      *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-    }
-    const uint32_t redo = __ballot_sync(0xffffffffu, again);
-#pragma unroll 1
     for (int h = 0; h < 2; ++h)
-      if (redo >> (16 * h) & 1u) {
-        int pr, qi;
-        p.row(s.qt, s.pair, r0 + h, pr, qi);
-        diff_row<__nv_bfloat16>(p.args, s.b, pr, qi, lam, sq[warp]);
-      }
+#pragma unroll
+      for (int y = 0; y < 2; ++y) q[h][y] = __ldcg(reinterpret_cast<const float4*>(at + (1 + (kV * h + ch) / 4 + y) * kPiece));
+    const bool none = k > begun && p.starts[k].tiles == 0;
+    const float pm[2] = {st.x, st.z}, pl[2] = {st.y, st.w};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (none || pm[h] == -INFINITY) continue;       // no keys of this row
+      const float mn = max3(m[h], pm[h], pm[h]), f = ex2(m[h] - mn), g = ex2(pm[h] - mn);
+      m[h] = mn;
+      l[h] = l[h] * f + pl[h] * g;
+      const float v[8] = {q[h][0].x, q[h][0].y, q[h][0].z, q[h][0].w, q[h][1].x, q[h][1].y, q[h][1].z, q[h][1].w};
+#pragma unroll
+      for (int y = 0; y < 8; ++y) acc[h][y] = acc[h][y] * f + v[y] * g;
+    }
   }
+  const bool any = reach.limit(i) > 0;
+  const float f0 = any ? 1.f / l[0] : 0.f, f1 = any ? -lam / l[1] : 0.f;
+  float x[8], ss = 0.f;
+#pragma unroll
+  for (int y = 0; y < 8; ++y) {
+    x[y] = acc[0][y] * f0 + acc[1][y] * f1;
+    ss = fmaf(x[y], x[y], ss);
+  }
+  ss += __shfl_xor_sync(0xffffffffu, ss, 16);
+  if (lane < kMergeRows) square[warp][row] = ss;
+  __syncthreads();                           // (all of a block comes here, or none of it)
+  ss = 0.f;
+#pragma unroll
+  for (int w = 0; w < kMergeWarps; ++w) ss += square[w][row];
+  const bool again = mine && !(ss < INFINITY);   // a part that says so, or values out of range
+  if (p.tail.norm_w) {
+    const float rn = (1.f - p.tail.lambda_init) * rsqrtf(ss * (1.f / kV) + p.tail.norm_eps);
+#pragma unroll
+    for (int y = 0; y < 8; y += 4) {
+      const float4 w = __ldg(reinterpret_cast<const float4*>(p.tail.norm_w + ch + y));
+      x[y] *= rn * w.x; x[y + 1] *= rn * w.y; x[y + 2] *= rn * w.z; x[y + 3] *= rn * w.w;
+    }
+  }
+  if (mine && !again) {
+    __nv_bfloat16* dst = p.o + (((size_t)s.b * 2 * p.pairs + 2 * pair + (ch >> 6)) * p.items.Nq + i) * kD + (ch & 63);
+    *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+  }
+  const uint32_t redo = __ballot_sync(0xffffffffu, again);     // (rows in bits 0 to 15, alike in all warps)
+  if (redo == 0) return;
+#pragma unroll 1
+  for (int h = warp; h < kMergeRows; h += kMergeWarps)
+    if (redo >> h & 1u) {
+      int pr, qi;
+      p.row(s.qt, s.pair, kMergeRows * blockIdx.y + h, pr, qi);
+      diff_row<__nv_bfloat16>(p.args, s.b, pr, qi, lam, sq[warp]);
+    }
 }
 
 }  // namespace

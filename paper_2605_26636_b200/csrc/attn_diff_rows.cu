@@ -2,9 +2,9 @@
 //
 // All queries of the pairs that share a pair of keys, at most 16 rows, are the M dimension of mma.sync m16n8k16: the work is reading K and
 // V once (512 bytes a key and pair), far below what needs tcgen05.  Keys come in boxes of 64 through a TMA ring of four (128 KB in
-// flight per SM) to eight warps: four take the even boxes, four the odd ones, 16 keys each, with fragments by ldmatrix from the
-// swizzled rows.  Every warp keeps its own running reference, sum and products (both maps, 16 x 128) in registers; the reference
-// moves when a score outgrows it by 2^8, which one vote per box decides.  At the end of an item the eight warps' results are summed
+// flight per SM) to sixteen warps: eight per map, four of them to the even boxes, four to the odd ones, 16 keys each, with fragments by
+// ldmatrix from the swizzled rows.  Every warp keeps its own running reference, sum and product (16 x 128) in registers; the reference
+// moves when a score outgrows it by 2^8, which one vote per box decides.  At the end of an item the warps' results are summed
 // through shared memory, and written, or left as a partial where the item goes on in another block (see attn_diff.cuh: blocks take
 // equal shares of all items' keys, so sequences of any lengths keep all SMs busy to the end).
 //
@@ -19,11 +19,13 @@ using namespace tc;
 using namespace diff;
 
 constexpr int kRows = 16;
+static_assert(kRows % kPartialRows == 0, "slots of whole groups of rows");
 constexpr int kBox = 64;                      // keys of a box
 constexpr int kStages = 4;
 constexpr int kBoxBytes = kBox * kD * 2;      // one head's: 8 KB
 constexpr int kStageBytes = 4 * kBoxBytes;    // K of both heads, V of both
-constexpr int kWorkers = 8;                   // warps that compute
+constexpr int kWorkers = 16;                  // warps that compute
+constexpr int kPerMap = kWorkers / 2;
 constexpr int kThreads = (kWorkers + 1) * 32;
 constexpr int kQStride = kV * 2 + 16;         // bytes between rows of queries: ldmatrix's eight rows in different banks
 constexpr int kSumStride = kV + 4;            // floats between rows of the warps' results: rows g and g + 1 in different banks
@@ -32,12 +34,12 @@ struct __align__(16) Shared {
   uint64_t full[kStages], empty[kStages];
   long long scan[34];
   Start start;
-  float m[kWorkers][2][kRows], l[kWorkers][2][kRows];
+  float m[2][kPerMap][kRows], l[2][kPerMap][kRows];
   volatile uint32_t abort_flag;
   uint32_t leave;                             // what the workers go by: one of them reads the flag for all
   __align__(16) unsigned char q[kRows][kQStride];
 };
-constexpr size_t kSumBytes = (size_t)kWorkers * kRows * kSumStride * 4;
+constexpr size_t kSumBytes = (size_t)kPerMap * kRows * kSumStride * 4;
 constexpr size_t kSmemBytes = kStages * (size_t)kStageBytes + kSumBytes + sizeof(Shared) + 1024;
 static_assert(kSmemBytes <= 227 * 1024, "shared memory of one block");
 
@@ -66,14 +68,14 @@ diff_rows_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant
     prefetch_map(&mapV);
   }
   unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  float* sums = reinterpret_cast<float*>(smem + kStages * kStageBytes);           // [warp][row][channel], one map at a time
+  float* sums = reinterpret_cast<float*>(smem + kStages * kStageBytes);           // [warp of a map][row][channel], one map at a time
   Shared* sh = reinterpret_cast<Shared*>(smem + kStages * kStageBytes + kSumBytes);
   const uint32_t ring = smem_u32(smem);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&sh->full[s], 1);
-      mbar_init(&sh->empty[s], 4);            // the four warps that read it
+      mbar_init(&sh->empty[s], 8);            // the eight warps that read it
     }
     sh->abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -130,15 +132,16 @@ diff_rows_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant
     return;
   }
 
-  // ================= eight warps =================
-  const int tr = threadIdx.x >> 4, tc = threadIdx.x & 15;     // where a thread has a row's eight channels: row tr, channels 8 tc ..
-  const int g = lane >> 2, t = lane & 3, half = warp >> 2, part = warp & 3;   // boxes n with n % 2 == half; keys 16 part .. of them
+  // ================= sixteen warps =================
+  const int g = lane >> 2, t = lane & 3;
+  const int part = warp & 3, m = (warp >> 2) & 1, half = warp >> 3;   // keys 16 part .. of the boxes n with n % 2 == half; map
+  const int mine = 4 * half + part;         // of the warps of the map
   const float lam = lambda_of(p.tail);
   const float sl2 = p.scale_log2;
   // ldmatrix addresses within a box: row (key) and 16-byte chunk of a lane, chunks swizzled by the row
   const int krow = 16 * part + (lane & 7) + ((lane & 16) >> 1), kchunk = (lane >> 3) & 1;    // x4: keys 0-7 | chunks 0, 1; keys 8-15 | chunks 0, 1
   const int vrow = 16 * part + (lane & 15), vchunk = lane >> 4;                              // x4: keys 0-7, 8-15 of chunk 0; of chunk 1
-  const uint32_t qaddr = smem_u32(&sh->q[lane & 15][16 * (lane >> 4)]);   // x4: rows 0-7, 8-15 of chunk 0; of chunk 1
+  const uint32_t qaddr = smem_u32(&sh->q[lane & 15][16 * (lane >> 4)]) + m * (kD * 2);   // x4: rows 0-7, 8-15 of chunk 0; of chunk 1
   uint32_t n = 0;
   bool ok = true;
   while (it.next(p.items)) {
@@ -153,92 +156,79 @@ diff_rows_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant
       p.row(0, it.ipair, g + 8 * h, pair, i);
       lim[h] = g + 8 * h < rows ? reach.limit(i) : 0;
     }
-    {                                         // queries of both maps, zeros past the rows: 16 bytes a thread
+    if (threadIdx.x < kRows * 16) {           // queries of both maps, zeros past the rows: 16 bytes a thread
+      const int r = threadIdx.x >> 4, c = threadIdx.x & 15;
       int pair, i;
-      p.row(0, it.ipair, tr, pair, i);
-      const __nv_bfloat16* q = (const __nv_bfloat16*)p.args.q + it.ib * p.args.qs.batch + (int64_t)i * p.args.qs.tok + (2 * pair + (tc >> 3)) * p.args.qs.head + 8 * (tc & 7);
-      *reinterpret_cast<uint4*>(&sh->q[tr][16 * tc]) = tr < rows ? *reinterpret_cast<const uint4*>(q) : make_uint4(0u, 0u, 0u, 0u);
-      workers_sync();
+      p.row(0, it.ipair, r, pair, i);
+      const __nv_bfloat16* q = (const __nv_bfloat16*)p.args.q + it.ib * p.args.qs.batch + (int64_t)i * p.args.qs.tok + (2 * pair + (c >> 3)) * p.args.qs.head + 8 * (c & 7);
+      *reinterpret_cast<uint4*>(&sh->q[r][16 * c]) = r < rows ? *reinterpret_cast<const uint4*>(q) : make_uint4(0u, 0u, 0u, 0u);
     }
+    workers_sync();
     const int least = p.items.causal ? reach.limit(0) : reach.len;      // keys that every row sees
-    float ref[2][2] = {{-INFINITY, -INFINITY}, {-INFINITY, -INFINITY}}, l[2][2] = {{0.f, 0.f}, {0.f, 0.f}};   // [map][row g, g + 8]
-    float acc[2][16][4];
+    float ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};           // rows g, g + 8
+    float acc[16][4];
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int j = 0; j < 16; ++j)
 #pragma unroll
-      for (int j = 0; j < 16; ++j)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) acc[m][j][c] = 0.f;
+      for (int c = 0; c < 4; ++c) acc[j][c] = 0.f;
 
     for (int x = first; x < last; ++x, ++n) {
       if ((int)(n & 1) != half) continue;
       const uint32_t s = n % kStages, base = ring + s * kStageBytes;
       ok = warp_wait(&sh->full[s], (n / kStages) & 1, &sh->abort_flag, p.status);
       if (!ok) break;
-      float sc[2][2][4];
+      float sc[2][4];
 #pragma unroll
-      for (int m = 0; m < 2; ++m) {
+      for (int c = 0; c < 4; ++c) sc[0][c] = sc[1][c] = 0.f;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) sc[m][0][c] = sc[m][1][c] = 0.f;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          uint32_t qa[4], b[4];               // b: keys 0-7: channels 16 k .., + 8; keys 8-15: the same
-          ldsm4(qa, qaddr + m * (kD * 2) + 32 * k);
-          ldsm4(b, base + m * kBoxBytes + krow * 128 + (((2 * k + kchunk) ^ (krow & 7)) << 4));
-          mma16816(sc[m][0], qa, b[0], b[1]);
-          mma16816(sc[m][1], qa, b[2], b[3]);
-        }
+      for (int k = 0; k < 4; ++k) {
+        uint32_t qa[4], b[4];                 // b: keys 0-7: channels 16 k .., + 8; keys 8-15: the same
+        ldsm4(qa, qaddr + 32 * k);
+        ldsm4(b, base + m * kBoxBytes + krow * 128 + (((2 * k + kchunk) ^ (krow & 7)) << 4));
+        mma16816(sc[0], qa, b[0], b[1]);
+        mma16816(sc[1], qa, b[2], b[3]);
       }
       const int key0 = x * kBox + 16 * part;
       const bool edge = key0 + 16 > least;    // some row does not see some key
       bool moves = false;
 #pragma unroll
-      for (int m = 0; m < 2; ++m)
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            float v = sc[m][j][c] * sl2;
-            if (edge && key0 + 8 * j + 2 * t + (c & 1) >= lim[c >> 1]) v = -INFINITY;
-            sc[m][j][c] = v;
-            moves |= !(v <= ref[m][c >> 1] + 8.f);
-          }
+        for (int c = 0; c < 4; ++c) {
+          float v = sc[j][c] * sl2;
+          if (edge && key0 + 8 * j + 2 * t + (c & 1) >= lim[c >> 1]) v = -INFINITY;
+          sc[j][c] = v;
+          moves |= !(v <= ref[c >> 1] + 8.f);
+        }
       if (__any_sync(0xffffffffu, moves)) {   // a score outgrows its row's reference, or is no number: the first box always
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+        for (int h = 0; h < 2; ++h) {
+          float mx = max3(max3(sc[0][2 * h], sc[0][2 * h + 1], sc[1][2 * h]), sc[1][2 * h + 1], ref[h]);
+          mx = max3(mx, __shfl_xor_sync(0xffffffffu, mx, 1), mx);
+          mx = max3(mx, __shfl_xor_sync(0xffffffffu, mx, 2), mx);
+          const float f = mx == -INFINITY ? 1.f : ex2(ref[h] - mx) + (mx - mx);    // +inf, no number: no number
+          ref[h] = mx;
+          l[h] *= f;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            float mx = max3(max3(sc[m][0][2 * h], sc[m][0][2 * h + 1], sc[m][1][2 * h]), sc[m][1][2 * h + 1], ref[m][h]);
-            mx = max3(mx, __shfl_xor_sync(0xffffffffu, mx, 1), mx);
-            mx = max3(mx, __shfl_xor_sync(0xffffffffu, mx, 2), mx);
-            const float f = mx == -INFINITY ? 1.f : ex2(ref[m][h] - mx) + (mx - mx);    // +inf, no number: no number
-            ref[m][h] = mx;
-            l[m][h] *= f;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              acc[m][j][2 * h] *= f;
-              acc[m][j][2 * h + 1] *= f;
-            }
-          }
-      }
-      // A fragments of the probabilities, those of map 0 (which weighs most) as two bf16 terms: the difference of the maps is smaller
-      // than either, and their roundings left o at 2.6e-3 of the exact result (its own rounding: 1.7e-3).  Both maps so: 1.64e-3, 92 us.
-      uint32_t pa[2][4], pb[4];
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const float r0 = ref[m][0] == -INFINITY ? 0.f : ref[m][0], r1 = ref[m][1] == -INFINITY ? 0.f : ref[m][1];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float p0 = ex2(sc[m][j][0] - r0), p1 = ex2(sc[m][j][1] - r0), p2 = ex2(sc[m][j][2] - r1), p3 = ex2(sc[m][j][3] - r1);
-          l[m][0] += p0 + p1;
-          l[m][1] += p2 + p3;
-          pa[m][2 * j] = pack_bf16(p0, p1);
-          pa[m][2 * j + 1] = pack_bf16(p2, p3);
-          if (m == 0) {
-            pb[2 * j] = rest_bf16(p0, p1, pa[m][2 * j]);
-            pb[2 * j + 1] = rest_bf16(p2, p3, pa[m][2 * j + 1]);
+          for (int j = 0; j < 16; ++j) {
+            acc[j][2 * h] *= f;
+            acc[j][2 * h + 1] *= f;
           }
         }
+      }
+      // A fragments of the probabilities, those of map 0 (which weighs most) as two bf16 terms: the difference of the maps is smaller
+      // than either, and their roundings left o at 2.6e-3 of the exact result (its own rounding: 1.7e-3; so 2.1e-3).
+      uint32_t pa[4], pb[4];
+      const float r0 = ref[0] == -INFINITY ? 0.f : ref[0], r1 = ref[1] == -INFINITY ? 0.f : ref[1];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float p0 = ex2(sc[j][0] - r0), p1 = ex2(sc[j][1] - r0), p2 = ex2(sc[j][2] - r1), p3 = ex2(sc[j][3] - r1);
+        l[0] += p0 + p1;
+        l[1] += p2 + p3;
+        pa[2 * j] = pack_bf16(p0, p1);
+        pa[2 * j + 1] = pack_bf16(p2, p3);
+        pb[2 * j] = rest_bf16(p0, p1, pa[2 * j]);
+        pb[2 * j + 1] = rest_bf16(p2, p3, pa[2 * j + 1]);
       }
       const bool behind = key0 + 16 > reach.len;   // rows of V that may hold anything: they count as zeros
       const int k0 = key0 + 2 * t;
@@ -251,63 +241,60 @@ diff_rows_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant
         if (behind) {
           b[0] &= keep0; b[1] &= keep1; b[2] &= keep0; b[3] &= keep1;
         }
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          mma16816(acc[m][j], pa[m], b[0], b[1]);
-          mma16816(acc[m][j + 1], pa[m], b[2], b[3]);
-          if (m == 0) {
-            mma16816(acc[m][j], pb, b[0], b[1]);
-            mma16816(acc[m][j + 1], pb, b[2], b[3]);
-          }
+        mma16816(acc[j], pa, b[0], b[1]);
+        mma16816(acc[j + 1], pa, b[2], b[3]);
+        if (m == 0) {
+          mma16816(acc[j], pb, b[0], b[1]);
+          mma16816(acc[j + 1], pb, b[2], b[3]);
         }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh->empty[s]);
     }
-    // ---- the eight warps' results.  (A wait that ran out leaves all of them, by the flag, before anybody waits for the others.)
+    // ---- the warps' results.  (A wait that ran out leaves all of them, by the flag, before anybody waits for the others.)
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        l[m][h] += __shfl_xor_sync(0xffffffffu, l[m][h], 1);
-        l[m][h] += __shfl_xor_sync(0xffffffffu, l[m][h], 2);
-        if (t == 0) {
-          sh->m[warp][m][g + 8 * h] = ref[m][h];
-          sh->l[warp][m][g + 8 * h] = l[m][h];
-        }
+    for (int h = 0; h < 2; ++h) {
+      l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+      l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+      if (t == 0) {
+        sh->m[m][mine][g + 8 * h] = ref[h];
+        sh->l[m][mine][g + 8 * h] = l[h];
       }
+    }
     workers_sync();
-    float M[2], total[2], res[2][8];
+    float f[2];
 #pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      M[m] = -INFINITY;
-      total[m] = 0.f;
+    for (int h = 0; h < 2; ++h) {
+      float top = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < kWorkers; ++w) M[m] = max3(M[m], sh->m[w][m][tr], M[m]);
+      for (int w = 0; w < kPerMap; ++w) top = max3(top, sh->m[m][w][g + 8 * h], top);
+      f[h] = ref[h] == -INFINITY ? 0.f : ex2(ref[h] - top);
+    }
+    // from here on a warp has row `warp`, four channels a lane
+    const int tr = warp, ch = 4 * lane;
+    float M[2], total[2], res[2][4];
 #pragma unroll
-      for (int w = 0; w < kWorkers; ++w) total[m] += sh->m[w][m][tr] == -INFINITY ? 0.f : sh->l[w][m][tr] * ex2(sh->m[w][m][tr] - M[m]);
-      float top[2] = {-INFINITY, -INFINITY};
+    for (int x = 0; x < 2; ++x) {
+      M[x] = -INFINITY;
+      total[x] = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWorkers; ++w)
+      for (int w = 0; w < kPerMap; ++w) M[x] = max3(M[x], sh->m[x][w][tr], M[x]);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) top[h] = max3(top[h], sh->m[w][m][g + 8 * h], top[h]);
+      for (int w = 0; w < kPerMap; ++w) total[x] += sh->m[x][w][tr] == -INFINITY ? 0.f : sh->l[x][w][tr] * ex2(sh->m[x][w][tr] - M[x]);
+      if (m == x)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float f = ref[m][h] == -INFINITY ? 0.f : ex2(ref[m][h] - top[h]);
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-          *reinterpret_cast<float2*>(sums + (warp * kRows + g + 8 * h) * kSumStride + 8 * j + 2 * t) = make_float2(acc[m][j][2 * h] * f, acc[m][j][2 * h + 1] * f);
-      }
+          for (int j = 0; j < 16; ++j)
+            *reinterpret_cast<float2*>(sums + (mine * kRows + g + 8 * h) * kSumStride + 8 * j + 2 * t) = make_float2(acc[j][2 * h] * f[h], acc[j][2 * h + 1] * f[h]);
       workers_sync();
 #pragma unroll
-      for (int y = 0; y < 8; ++y) res[m][y] = 0.f;
+      for (int y = 0; y < 4; ++y) res[x][y] = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWorkers; ++w)
-#pragma unroll
-        for (int y = 0; y < 8; y += 4) {
-          const float4 v = *reinterpret_cast<const float4*>(sums + (w * kRows + tr) * kSumStride + 8 * tc + y);
-          res[m][y] += v.x; res[m][y + 1] += v.y; res[m][y + 2] += v.z; res[m][y + 3] += v.w;
-        }
+      for (int w = 0; w < kPerMap; ++w) {
+        const float4 v = *reinterpret_cast<const float4*>(sums + (w * kRows + tr) * kSumStride + ch);
+        res[x][0] += v.x; res[x][1] += v.y; res[x][2] += v.z; res[x][3] += v.w;
+      }
       if (threadIdx.x == 0) sh->leave = sh->abort_flag;
       workers_sync();                         // (the other map's turn, or the next item's)
     }
@@ -315,36 +302,31 @@ diff_rows_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant
       if (threadIdx.x == 0) p.starts[blockIdx.x].left = 1;
       break;
     }
+    if (tr >= rows) continue;
     if (!it.whole()) {
-      if (tr >= rows) continue;
-      float* dst = p.partial + ((size_t)partial_slot(blockIdx.x, it.t0) * kRows + tr) * kPartial;
-      if (tc == 0) *reinterpret_cast<float4*>(dst) = make_float4(M[0], total[0], M[1], total[1]);
+      float* dst = p.partial + partial_at((size_t)partial_slot(blockIdx.x, it.t0) * kRows + tr);
+      if (lane == 0) *reinterpret_cast<float4*>(dst) = make_float4(M[0], total[0], M[1], total[1]);
 #pragma unroll
-      for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int y = 0; y < 8; y += 4)
-          *reinterpret_cast<float4*>(dst + 4 + kV * m + 8 * tc + y) = make_float4(res[m][y], res[m][y + 1], res[m][y + 2], res[m][y + 3]);
+      for (int x = 0; x < 2; ++x) *reinterpret_cast<float4*>(dst + (1 + (kV * x + ch) / 4) * kPiece) = make_float4(res[x][0], res[x][1], res[x][2], res[x][3]);
       continue;
     }
     int pair, i;
     p.row(0, it.ipair, tr, pair, i);
     const bool any = reach.limit(i) > 0;      // (a row that sees keys, none of weight: 0 / 0)
     const float f0 = 1.f / total[0], f1 = -lam / total[1];
-    float xv[8], ss = 0.f;
+    float xv[4], ss = 0.f;
 #pragma unroll
-    for (int y = 0; y < 8; ++y) {
+    for (int y = 0; y < 4; ++y) {
       xv[y] = any ? res[0][y] * f0 + res[1][y] * f1 : 0.f;
       ss = fmaf(xv[y], xv[y], ss);
     }
     if (p.tail.norm_w) {
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);          // the 16 lanes of a row
-      const float rn = (1.f - p.tail.lambda_init) * rsqrtf(ss * (1.f / kV) + p.tail.norm_eps);
-#pragma unroll
-      for (int y = 0; y < 8; ++y) xv[y] *= rn * __ldg(p.tail.norm_w + 8 * tc + y);
+      const float rn = (1.f - p.tail.lambda_init) * rsqrtf(warp_sum(ss) * (1.f / kV) + p.tail.norm_eps);
+      const float4 w = __ldg(reinterpret_cast<const float4*>(p.tail.norm_w + ch));
+      xv[0] *= rn * w.x; xv[1] *= rn * w.y; xv[2] *= rn * w.z; xv[3] *= rn * w.w;
     }
-    __nv_bfloat16* dst = p.o + (((size_t)it.ib * 2 * p.pairs + 2 * pair + (tc >> 3)) * p.items.Nq + i) * kD + 8 * (tc & 7);
-    if (tr < rows) *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16(xv[0], xv[1]), pack_bf16(xv[2], xv[3]), pack_bf16(xv[4], xv[5]), pack_bf16(xv[6], xv[7]));
+    __nv_bfloat16* dst = p.o + (((size_t)it.ib * 2 * p.pairs + 2 * pair + (ch >> 6)) * p.items.Nq + i) * kD + (ch & 63);
+    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(xv[0], xv[1]), pack_bf16(xv[2], xv[3]));
   }
 }
 
