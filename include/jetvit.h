@@ -10,6 +10,9 @@
  *   F  full softmax attention (Eq. 1);
  *   S  a per-layer L/W/F schedule over a stack of independent layers
  *      (Sec. 3.2.3, Fig. 1b).
+ * Beside them: the projections either side of a mixer, the layer norm in front of
+ * them and its gradient, and two further mixers with their serving forms,
+ * differential attention and the selective scan with its short convolution.
  *
  * Conventions shared by every call
  *   Tensors   q, k, v, o are DEVICE pointers to [B, H, N, D] contiguous arrays,
@@ -270,7 +273,7 @@ jv_status jv_out_proj(const void* o, const void* w, const float* bias, void* y, 
  * The forward pass writes mean and rstd if they are not NULL (both or neither); the gradient reads them.  dw or db NULL: not
  * wanted; with both NULL no scratch is needed.
  * rows > 0, 0 < C <= 16384, eps >= 0.  Any alignment to the element is served; where every row and vector starts on a 16-byte boundary,
- * 16 bytes at a time.  Outputs share no byte with an input or each other.  Arithmetic in fp32, statistics of the centred
+ * 16 bytes at a time (faster).  Outputs share no byte with an input or each other.  Arithmetic in fp32, statistics of the centred
  * values; dw and db are summed in a fixed order (results repeat bit for bit).
  * jv_layer_norm_grad_workspace_bytes() sizes ws (256-byte aligned); 0 on invalid arguments.
  */
@@ -301,12 +304,15 @@ jv_status jv_layer_norm_grad(const void* dy, const void* x, const float* w, cons
  *   kv_len  device int32 [B] or NULL: keys j >= kv_len[b] do not exist (Nk bounds it, below 0 counts as 0).  Their memory may
  *           hold anything.
  *   causal  query i sees the keys j <= q_pos[b] + i only; q_pos device int32 [B] or NULL: Nk - Nq, the queries being the last of
- *           the Nk positions (0 for a whole prompt).  A key that a query does not see weighs exactly nothing or less than 2^-125
- *           of what it does see, so finite values of v do not reach it; infinities and NaN among the rows of v below kv_len may.
+ *           the Nk positions (0 for a whole prompt); any value is served.  A key that a query does not see weighs exactly nothing, so
+ *           finite values of v do not reach it; infinities and NaN among the rows of v below kv_len may (0 times infinity).
  * All rows of o are written.  A query that sees no key gets zeros.  As everywhere in this library a key of score -inf weighs
  * nothing, a row that sees keys but none of weight is NaN, and a score of +inf or NaN makes its row NaN.
- * bf16 tensors with D = 64: tensor cores, fp32 softmax and sums, one rounding of P to bf16 and one of o.  f32, and bf16 with other
- * D <= 64: fp32 arithmetic (row * element size a multiple of 16 bytes).  scale <= 0 selects 1/sqrt(D).
+ * bf16 tensors with D = 64: tensor cores, fp32 softmax and sums; P rounded to bf16, in map 0 (which weighs most) partly or wholly as two
+ * bf16 terms; one rounding of o.  Tiles of queries take exponentials against the largest score of 64 of a row's keys; a row whose later
+ * scores lie 41 or more above it, or whose sums leave the range of fp32, is computed again in fp32 within the call: exact,
+ * but slow where many rows are so.  Such calls obey the status word (Errors above).  f32, and bf16 with other D <= 64: fp32 arithmetic,
+ * one warp per row (rows of multiples of 16 bytes).  scale <= 0 selects 1/sqrt(D).
  * Few queries (single tokens against a cache) and prompts take different kernels; both spread the keys over the whole GPU whatever
  * the lengths are.  ws must cover jv_diff_attn_workspace_bytes() (0 on invalid arguments), 256-byte aligned.
  */
@@ -353,7 +359,8 @@ jv_status jv_causal_conv(const void* x, const float* w, const float* bias, const
  * u, dt, z are [B, L, C], Bm and Cm [B, L, Ns] (shared by the channels), y [B, L, C] contiguous, all of shape.dtype; A fp32 [C, Ns],
  * D and dt_bias fp32 [C] or NULL, z NULL: no gate.  The strides are elements between {token rows, batch elements} (0: contiguous
  * rows; L rows).  state_in fp32 [B, C, Ns] or NULL (zeros), state_out receives the state behind the last token if not
- * NULL; it may be state_in itself.  lens as for jv_causal_conv.  1 <= Ns <= 64.  States and sums in fp32.
+ * NULL; it may be state_in itself.  lens as for jv_causal_conv.  1 <= Ns <= 64.  States and sums in fp32.  An A of minus infinity
+ * forgets within a step; a step d of 0 leaves the state as it is for any A.
  * Long sequences of few channels are cut into chunks whose states pass through ws (jv_selective_scan_workspace_bytes(), 0 where none is
  * needed or the arguments are invalid; 256-byte aligned).  L = 1 is the single-token form.
  */

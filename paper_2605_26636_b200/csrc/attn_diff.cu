@@ -16,7 +16,7 @@
 // is not finite, is marked, and done again by the second launch, exactly and slowly, from the inputs (so are infinities and NaN among
 // them).  That takes a score 41 above, or below, every one of the first 64 keys; it saves the maximum of every other
 // step, and its order between the sets: half of a step's instructions.  The exponentials are all the MUFU unit's: it gives 0 for a key
-// that scores -inf, and two of eight by a polynomial are no faster (651 us against 661, where the kernel is bound as below).
+// that scores -inf, and two of eight by a polynomial are no faster (B = 4, 8 pairs, 73 x 73 tokens, without second terms: 651 us, 661).
 //
 // What bounds a step is the chain of the warps that issue for it: beside four busy softmax warps in its sub-core an instruction takes such a
 // warp some 8 clocks, a look at a barrier 110 and more.  Scores and products from one warp per map, each phase elected and
@@ -25,11 +25,14 @@
 //
 // The difference of the maps is smaller than either: bf16 probabilities left o at 2.6e-3 of the exact result (its own rounding: 1.7e-3).
 // So map 0, which weighs most, has its probabilities of kLoKeys of every 64 keys as two bf16 terms: what the rounding took off them
-// goes through shared memory (tensor memory is full) into products of their own, 2.3e-3.
+// goes through shared memory (tensor memory is full) into products of their own: 2.4e-3, and 652 us become 735 at 73 x 73 tokens.
 //
 // Behind an item's last key each of a row's four threads takes 32 channels from both accumulators: the sums and the shares of
 // the row's mean square are exchanged through shared memory, the difference is normalised and written.  Parts of an item (see
 // attn_diff.cuh) go to the workspace as they are.
+//
+// Measured, with the launch that merges: B = 4, 8 pairs, 73 x 73 tokens 735 us (850 at the power cap; 698 GF: 950 TF), two causal prompts
+// of 4096 tokens, 8 pairs, 127 us, 256 queries against 16384 keys, 8 pairs, 48 us.
 //
 // Keys that a row does not see are set to -inf behind the load of the scores; rows of V that lie behind a length may hold anything, and
 // are overwritten with zeros in shared memory before the first product of their tile.
@@ -534,7 +537,7 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
 // Blocks of a call, one per SM at most: one for every item, or for every kTilesMin tiles of the longest that the items can be
 constexpr int kTilesMin = 4;
 // An item costs as much as four tiles beside its own (first scores, epilogue).  Measured, in units of 1 / 2 / 3 / 4 / 6 tiles: two
-// causal prompts of 4096 tokens, 8 pairs, 176 / 143 / 125 / 124 / 128 us, with none 231; 73 x 73 tokens 658 to 664, 6: 694.
+// causal prompts of 4096 tokens, 8 pairs, 173 / 137 / 127 / 127 / 132 us; 73 x 73 tokens 744 to 784 either way.
 constexpr int kLead = 4, kWhole = 2;
 int diff_blocks(int B, int pairs, int Nq, int Nk) {
   const int64_t items = (int64_t)B * pairs * ceil_div(Nq, kTile), tiles = items * ceil_div(Nk, kTile);
