@@ -238,9 +238,20 @@ __global__ void __launch_bounds__(kGradWarps * 32, 1) layer_norm_grad_rows_kerne
   for (int s = 0; s < kStages - 1; ++s) fetch(first + s * step, s);
   const float inv_c = 1.f / (float)p.C;
   int stage = 0;
+  // a row's statistics are loaded a row ahead, too (where they were needed at once every warp waited for them, row after row: 32768 rows
+  // of 1024 bf16 values 46.9 us, now 40.0; 21316 of 768 fp32 36.0, now 34.6)
+  float mean_next = 0.f, rstd_next = 0.f;
+  auto statistics = [&](int64_t row) {
+    if (row < p.rows) {
+      mean_next = __ldg(p.mean + row);
+      rstd_next = __ldg(p.rstd + row);
+    }
+  };
+  statistics(first);
   for (int64_t row = first; row < p.rows; row += step) {
     fetch(row + (kStages - 1) * step, stage == 0 ? kStages - 1 : stage - 1);
-    const float mean = __ldg(p.mean + row), rstd = __ldg(p.rstd + row);
+    const float mean = mean_next, rstd = rstd_next;
+    statistics(row + step);
     const uint64_t nmean2 = pack2(-mean, -mean), rstd2 = pack2(rstd, rstd);
     asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
     const unsigned char* at = mine + stage * 2 * NCH * 512;
@@ -421,9 +432,11 @@ __global__ void __launch_bounds__(BLOCK ? 512 : 128, 1) layer_norm_grad_kernel(c
   }
 }
 
-// Column sums of the blocks' partials [n, 2, C]: 32 columns a block, eight threads a column
-__global__ void __launch_bounds__(256) layer_norm_sum_kernel(const float* __restrict__ partial, int n, int C, float* dw, float* db) {
-  __shared__ float red[8][33];
+// Column sums of the blocks' partials [n, 2, C]: 32 columns a block, kSumParts threads a column (a call of 32768 rows of 1024 with 8 / 16:
+// 41.3 / 40.0 us)
+constexpr int kSumParts = 16;
+__global__ void __launch_bounds__(kSumParts * 32) layer_norm_sum_kernel(const float* __restrict__ partial, int n, int C, float* dw, float* db) {
+  __shared__ float red[kSumParts][33];
   griddep_wait();
   griddep_launch_dependents();
   const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
@@ -431,14 +444,14 @@ __global__ void __launch_bounds__(256) layer_norm_sum_kernel(const float* __rest
   float s = 0.f;
   if (c < 2 * C) {
 #pragma unroll 8
-    for (int i = part; i < n; i += 8) s += __ldcg(partial + (size_t)i * 2 * C + c);
+    for (int i = part; i < n; i += kSumParts) s += __ldcg(partial + (size_t)i * 2 * C + c);
   }
   red[part][lane] = s;
   __syncthreads();
   if (part == 0 && c < 2 * C) {
     s = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += red[i][lane];
+    for (int i = 0; i < kSumParts; ++i) s += red[i][lane];
     if (c < C) {
       if (dw) dw[c] = s;
     } else if (db) {
@@ -534,7 +547,7 @@ cudaError_t launch_layer_norm_grad(const NormArgs& a, float* partial, float* dw,
   const NormParams p{a.x, a.dy, a.w, nullptr, a.y, a.mean, a.rstd, sums ? partial : nullptr, a.rows, a.x_stride, a.dy_stride, a.C, 0.f};
   const cudaError_t e = dispatch_norm<true>(a, p, blocks, st);
   if (e != cudaSuccess || !sums) return e;
-  return launch_programmatic(layer_norm_sum_kernel, dim3((unsigned)ceil_div(2 * a.C, 32)), 256, 0, st, (const float*)partial, blocks, a.C, dw, db);
+  return launch_programmatic(layer_norm_sum_kernel, dim3((unsigned)ceil_div(2 * a.C, 32)), kSumParts * 32, 0, st, (const float*)partial, blocks, a.C, dw, db);
 }
 
 }  // namespace jv
