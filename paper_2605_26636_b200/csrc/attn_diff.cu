@@ -514,7 +514,8 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
           }
           uint32_t pk[4];
 #pragma unroll
-          for (int y = 0; y < 4; ++y) pk[y] = pack_bf16(out[8 * c + 2 * y] * rn * w[2 * y], out[8 * c + 2 * y + 1] * rn * w[2 * y + 1]);
+          for (int y = 0; y < 4; ++y)           // (no key: 0 whatever the norm makes of zeros)
+            pk[y] = limit > 0 ? pack_bf16(out[8 * c + 2 * y] * rn * w[2 * y], out[8 * c + 2 * y + 1] * rn * w[2 * y + 1]) : 0u;
           *reinterpret_cast<uint4*>(dst + 8 * c) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
         }
       }

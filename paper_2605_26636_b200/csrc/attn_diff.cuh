@@ -278,7 +278,10 @@ __device__ __forceinline__ void diff_row(const DiffArgs& a, int b, int p, int i,
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
     const int c = lane + 32 * j;
-    if (c < 2 * D) from_f32(o + (c / D) * (int64_t)a.Nq * D + c % D, a.norm_w ? x[j] * r * __ldg(a.norm_w + c) : x[j]);
+    if (c < 2 * D) {
+      const float y = a.norm_w ? x[j] * r * __ldg(a.norm_w + c) : x[j];
+      from_f32(o + (c / D) * (int64_t)a.Nq * D + c % D, limit > 0 ? y : 0.f);      // (no key: 0 whatever the norm makes of zeros)
+    }
   }
 }
 

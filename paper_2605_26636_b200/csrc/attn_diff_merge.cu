@@ -113,6 +113,9 @@ __global__ void __launch_bounds__(kMergeWarps * 32, 4) diff_merge_kernel(const D
       x[y] *= rn * w.x; x[y + 1] *= rn * w.y; x[y + 2] *= rn * w.z; x[y + 3] *= rn * w.w;
     }
   }
+  if (!any)
+#pragma unroll
+    for (int y = 0; y < 8; ++y) x[y] = 0.f;  // (whatever the norm makes of zeros)
   if (mine && !again) {
     __nv_bfloat16* dst = p.o + (((size_t)s.b * 2 * p.pairs + 2 * pair + (ch >> 6)) * p.items.Nq + i) * kD + (ch & 63);
     *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));

@@ -327,6 +327,7 @@ diff_rows_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant
       const float4 w = __ldg(reinterpret_cast<const float4*>(p.tail.norm_w + ch));
       xv[0] *= rn * w.x; xv[1] *= rn * w.y; xv[2] *= rn * w.z; xv[3] *= rn * w.w;
     }
+    if (!any) xv[0] = xv[1] = xv[2] = xv[3] = 0.f;   // (whatever the norm makes of zeros)
     __nv_bfloat16* dst = p.o + (((size_t)it.ib * 2 * p.pairs + 2 * pair + (ch >> 6)) * p.items.Nq + i) * kD + (ch & 63);
     *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(xv[0], xv[1]), pack_bf16(xv[2], xv[3]));
   }

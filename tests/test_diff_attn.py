@@ -123,6 +123,25 @@ def test_lengths_positions_and_garbage_behind_them(Nq, Nk, causal):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("H,Nq,Nk,dtype,D", [(4, 1, 700, torch.bfloat16, 64), (4, 9, 700, torch.bfloat16, 64), (4, 200, 2000, torch.bfloat16, 64),
+                                             (300, 128, 128, torch.bfloat16, 64), (4, 40, 90, torch.float32, 64), (4, 40, 90, torch.bfloat16, 32)])
+def test_rows_without_keys_are_zeros_whatever_the_norm_makes_of_them(H, Nq, Nk, dtype, D):
+    """A norm without eps, and with a weight of infinity: 0 times infinity in rows that see no key.  Few queries, tiles in parts and whole,
+    fp32 arithmetic."""
+    q, k, v, lam, w = _tensors(2, H, H, Nq, Nk, D, dtype)
+    lens = torch.tensor([0, Nk], dtype=torch.int32, device="cuda")
+    pos = torch.tensor([-Nq // 2, -Nq], dtype=torch.int32, device="cuda")
+    some = (Nq + 1) // 2                                      # rows of the first sequence ahead of its first key
+    for top in (1.0, math.inf):
+        w[3] = top
+        call = lambda **kw: jv.diff_attn(q, k, v, lam, 0.8, norm_weight=w, norm_eps=0.0, **kw)
+        o = call(kv_len=lens)
+        assert (o[0] == 0).all() and torch.isfinite(o[1, 1::2]).all() and (o[1] != 0).any()
+        o = call(causal=True, q_pos=pos)
+        assert (o[1] == 0).all() and (o[0, :, :some] == 0).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("Nq,Nk,dtype", [(1, 700, torch.bfloat16), (200, 700, torch.bfloat16), (5, 90, torch.float32)])
 def test_positions_at_the_ends_of_their_type(Nq, Nk, dtype):
     q, k, v, lam, w = _tensors(5, 4, 2, Nq, Nk, dtype=dtype)
