@@ -498,7 +498,9 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
       if (i < p.items.Nq) {
         const float square = (bar->square[0][r] + bar->square[1][r]) + (bar->square[2][r] + bar->square[3][r]);
         if (set == 0) {
-          const bool again = limit > 0 && !(fine(s0) && fine(s1) && square < INFINITY);
+          // (with a norm also where the mean square is not safely within fp32)
+          const bool good = p.tail.norm_w ? square_fine(square * (1.f / kV) + p.tail.norm_eps) : square < INFINITY;
+          const bool again = limit > 0 && !(fine(s0) && fine(s1) && good);
           p.mark[((size_t)it.ib * p.pairs + it.ipair) * p.items.Nq + i] = again ? 1 : 0;
           if (again) bar->redo = 1;
         }

@@ -209,6 +209,33 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return d;
 }
 
+// The norm of a row: x times what this returns is x / sqrt(mean x^2 + eps).  A warp holds the row, N values a lane, inv_n = 1 / (their
+// number).  Where the mean square is not safely within fp32, x is scaled by a power of two first (values from 2^-149 to 2^128 then have
+// squares from 2^-98 to 2^96), and eps with it.
+constexpr float kSquareMin = 1e-30f;        // smallest mean square that is taken as it is
+__device__ __forceinline__ bool square_fine(float ms) { return ms >= kSquareMin && ms < INFINITY; }
+template <int N>
+__device__ __forceinline__ float inverse_rms(float (&x)[N], float inv_n, float eps) {
+  auto mean_square = [&](float e) {
+    float ss = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) ss = fmaf(x[j], x[j], ss);
+    return fmaf(warp_sum(ss), inv_n, e);
+  };
+  const float ms = mean_square(eps);
+  if (square_fine(ms)) return rsqrtf(ms);
+  float top = 0.f;
+#pragma unroll
+  for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(x[j]));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (!(top > 0.f && top < INFINITY)) return rsqrtf(ms);      // zeros; an infinity (no numbers stay so either way)
+  const float s = top > 1.f ? 0x1p-80f : 0x1p+100f;
+#pragma unroll
+  for (int j = 0; j < N; ++j) x[j] *= s;
+  return rsqrtf(mean_square(eps * s * s));
+}
+
 // One query row of one pair, by a whole warp, in fp32: a lane takes a key of 32 for the scores of both maps, then 2 D / 32 channels for
 // the products.  sq: 2 D floats of shared memory of the warp.
 template <typename T>
@@ -267,13 +294,10 @@ __device__ __forceinline__ void diff_row(const DiffArgs& a, int b, int p, int i,
     }
   }
   // a row that sees no key is 0; one whose keys all weigh nothing is no number (0 / 0)
-  float x[kPer], ss = 0.f;
+  float x[kPer];
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    x[j] = limit > 0 ? acc[0][j] / l[0] - lam * (acc[1][j] / l[1]) : 0.f;
-    if (lane + 32 * j < 2 * D) ss = fmaf(x[j], x[j], ss);
-  }
-  const float r = a.norm_w ? (1.f - a.lambda_init) * rsqrtf(warp_sum(ss) / (2 * D) + a.norm_eps) : 1.f;
+  for (int j = 0; j < kPer; ++j) x[j] = limit > 0 && lane + 32 * j < 2 * D ? acc[0][j] / l[0] - lam * (acc[1][j] / l[1]) : 0.f;
+  const float r = a.norm_w ? (1.f - a.lambda_init) * inverse_rms(x, 1.f / (float)(2 * D), a.norm_eps) : 1.f;
   T* o = (T*)a.o + (((int64_t)b * 2 * a.pairs + 2 * p) * a.Nq + i) * D;
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {

@@ -104,7 +104,8 @@ __global__ void __launch_bounds__(kMergeWarps * 32, 4) diff_merge_kernel(const D
   ss = 0.f;
 #pragma unroll
   for (int w = 0; w < kMergeWarps; ++w) ss += square[w][row];
-  const bool again = mine && !(ss < INFINITY);   // a part that says so, or values out of range
+  // a part that says so, values out of range, or (with a norm) a mean square that is not safely within fp32
+  const bool again = mine && any && !(p.tail.norm_w ? square_fine(ss * (1.f / kV) + p.tail.norm_eps) : ss < INFINITY);
   if (p.tail.norm_w) {
     const float rn = (1.f - p.tail.lambda_init) * rsqrtf(ss * (1.f / kV) + p.tail.norm_eps);
 #pragma unroll

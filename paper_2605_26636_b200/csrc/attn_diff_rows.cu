@@ -316,14 +316,11 @@ diff_rows_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant
     p.row(0, it.ipair, tr, pair, i);
     const bool any = reach.limit(i) > 0;      // (a row that sees keys, none of weight: 0 / 0)
     const float f0 = 1.f / total[0], f1 = -lam / total[1];
-    float xv[4], ss = 0.f;
+    float xv[4];
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      xv[y] = any ? res[0][y] * f0 + res[1][y] * f1 : 0.f;
-      ss = fmaf(xv[y], xv[y], ss);
-    }
+    for (int y = 0; y < 4; ++y) xv[y] = any ? res[0][y] * f0 + res[1][y] * f1 : 0.f;
     if (p.tail.norm_w) {
-      const float rn = (1.f - p.tail.lambda_init) * rsqrtf(warp_sum(ss) * (1.f / kV) + p.tail.norm_eps);
+      const float rn = (1.f - p.tail.lambda_init) * inverse_rms(xv, 1.f / kV, p.tail.norm_eps);
       const float4 w = __ldg(reinterpret_cast<const float4*>(p.tail.norm_w + ch));
       xv[0] *= rn * w.x; xv[1] *= rn * w.y; xv[2] *= rn * w.z; xv[3] *= rn * w.w;
     }

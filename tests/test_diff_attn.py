@@ -286,6 +286,15 @@ def test_scores_that_outgrow_the_first_keys(H, Nq, Nk):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("size,eps", [(1e22, 1e-5), (1e25, 0.0), (1e-25, 0.0), (1e-18, 1e-38)])
+@pytest.mark.parametrize("H,Nq,Nk,dtype,D", [(4, 1, 700, torch.bfloat16, 64), (2, 1, 70, torch.bfloat16, 64), (4, 200, 2000, torch.bfloat16, 64),
+                                             (300, 128, 128, torch.bfloat16, 64), (4, 40, 90, torch.float32, 64), (4, 40, 90, torch.bfloat16, 32)])
+def test_norms_of_rows_whose_squares_leave_fp32(H, Nq, Nk, dtype, D, size, eps):
+    q, k, v, lam, w = _tensors(2, H, H, Nq, Nk, D, dtype)
+    _check(q, k, (v.float() * size).to(dtype), lam, w, eps=eps, rms=False)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("Nq", [1, 130])
 def test_calls_while_the_status_word_is_set(Nq):
     q, k, v, lam, w = _tensors(3, 4, 4, Nq, 1700, seed=8)
