@@ -360,7 +360,7 @@ jv_status jv_causal_conv(const void* x, const float* w, const float* bias, const
  * D and dt_bias fp32 [C] or NULL, z NULL: no gate.  The strides are elements between {token rows, batch elements} (0: contiguous
  * rows; L rows).  state_in fp32 [B, C, Ns] or NULL (zeros), state_out receives the state behind the last token if not
  * NULL; it may be state_in itself.  lens as for jv_causal_conv.  1 <= Ns <= 64.  States and sums in fp32.  An A of minus infinity
- * forgets within a step; a step d of 0 leaves the state as it is for any A.
+ * forgets within a step; a step d of 0 leaves the state as it is for any A that is a number or an infinity.
  * Long sequences of few channels are cut into chunks whose states pass through ws (jv_selective_scan_workspace_bytes(), 0 where none is
  * needed or the arguments are invalid; 256-byte aligned).  L = 1 is the single-token form.
  */

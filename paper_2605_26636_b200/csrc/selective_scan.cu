@@ -59,11 +59,11 @@ __device__ __forceinline__ float silu(float x) { return __fdividef(x, 1.f + ex2(
 
 __device__ __forceinline__ int length_of(const ScanArgs& a, int b) { return a.lens ? min(max(__ldg(a.lens + b), 0), a.L) : a.L; }
 
-// A coefficient, for powers of 2.  Minus infinity (a state that is forgotten at once) as the lowest number: a step of 0, as tokens and chunks
-// past the end have it, then leaves the state alone, as it does elsewhere.
+// A coefficient, for powers of 2.  Infinities (minus: a state that is forgotten at once) as the numbers farthest from 0: a step of 0, as
+// tokens and chunks past the end have it, then leaves the state alone, as it does elsewhere.
 __device__ __forceinline__ float coefficient(float A) {
-  const float a = A * kLog2e;
-  return a < -3.4028235e38f ? -3.4028235e38f : a;
+  const float a = A * kLog2e, most = 3.4028235e38f;
+  return a < -most ? -most : a > most ? most : a;          // (no number stays none)
 }
 // A channel's coefficients and states: state n of lane s is s * NPL + n; states past Ns are zeros all through
 template <int NPL>

@@ -241,6 +241,20 @@ def test_states_that_are_forgotten_at_once(B, L, C, Ns, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("B,L,C,Ns", [(2, 1, 100, 16), (2, 4, 100, 16), (2, 37, 5000, 16), (3, 1000, 64, 16), (2, 600, 100, 33)])
+def test_steps_of_nothing_leave_the_state_for_any_A(B, L, C, Ns, dtype):
+    """A of either infinity with steps of 0, and with sequences that end inside a tile or ahead of a chunk."""
+    i = _scan_inputs(B, L, C, Ns, dtype)
+    i["A"][:, 1::3], i["A"][:, 2::3] = math.inf, -math.inf
+    i["dt"], i["dt_bias"] = torch.full_like(i["dt"], -200.0), None                 # softplus: exactly 0
+    lens = torch.tensor([max(1, L - 401 * b) for b in range(B)], dtype=torch.int32, device="cuda")
+    h, y = torch.empty_like(i["state"]), torch.zeros(B, L, C, dtype=dtype, device="cuda")
+    jv.selective_scan(**i, lens=lens, out=y, state_out=h)
+    assert torch.equal(h, i["state"]) and torch.isfinite(y).all()
+
+
+@pytest.mark.gpu
 def test_results_on_another_stream_do_not_lie_where_earlier_work_still_writes():
     i = _scan_inputs(1, 1000, 256, 16, torch.float32)
     w = torch.randn(256, 4, device="cuda")
