@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(kThreads) scan_step_kernel(const ScanArgs a) {
     float y = 0.f;
 #pragma unroll
     for (int n = 0; n < NPL; ++n) {
-      h[n] = fmaf(ex2(d * A2[n]), h[n], du * bm[n]);
+      h[n] = s * NPL + n < a.Ns ? fmaf(ex2(d * A2[n]), h[n], du * bm[n]) : 0.f;     // (0 times an infinite d or d u is no number)
       y = fmaf(h[n], cm[n], y);
     }
     y += __shfl_xor_sync(0xffffffffu, y, 1);
@@ -326,8 +326,9 @@ __device__ __forceinline__ void stage_tiles(const ScanArgs& a, Smem<T, S, NPL>* 
   }
 }
 
-// S lanes a channel, NPL states a lane.  kY: the whole thing; else the chunk's own state from zero and the sum of its steps only
-template <typename T, int S, int NPL, bool WIDE, bool kY>
+// S lanes a channel, NPL states a lane.  kY: the whole thing; else the chunk's own state from zero and the sum of its steps only.
+// kPad: there are states past Ns, to be kept at zero where d or d u are infinite (0 times that is no number); without kY they reach nothing.
+template <typename T, int S, int NPL, bool WIDE, bool kY, bool kPad>
 __global__ void __launch_bounds__(kThreads + kStagers, S == 4 && NPL <= 4 ? 2 : 1) scan_kernel(const ScanArgs a, int chunk, int nchunk, float* ws_state, float* ws_sum) {
   using Sm = Smem<T, S, NPL>;
   constexpr int kCh = Sm::kCh, kTT = Sm::kTT;
@@ -356,6 +357,7 @@ __global__ void __launch_bounds__(kThreads + kStagers, S == 4 && NPL <= 4 ? 2 : 
     A2p[n] = pack2(A2[2 * n], A2[2 * n + 1]);
     hp[n] = pack2(h[2 * n], h[2 * n + 1]);
   }
+  auto keep = [&](int n) { return s * NPL + n < a.Ns ? 0xffffffffu : 0u; };
   for (int i = 0; i < tiles; ++i) {
     Sm& sm = buf[i & 1];
     const int t0 = t_begin + i * kTT;
@@ -371,6 +373,7 @@ __global__ void __launch_bounds__(kThreads + kStagers, S == 4 && NPL <= 4 ? 2 : 
         if (!kY) sum += q.x;
         if constexpr (NPL == 1) {
           h[0] = fmaf(ex2(q.x * A2[0]), h[0], q.y * bc[0]);
+          if (kPad) h[0] = __uint_as_float(__float_as_uint(h[0]) & keep(0));
           if (kY) y[j] = h[0] * bc[1];
         } else {
           constexpr int kUse = kY ? 2 * NPL : NPL;              // B, and C
@@ -402,6 +405,7 @@ __global__ void __launch_bounds__(kThreads + kStagers, S == 4 && NPL <= 4 ? 2 : 
             float e0, e1;
             unpack2(mul2(dd, A2p[n]), e0, e1);
             hp[n] = fma2(pack2(ex2(e0), ex2(e1)), hp[n], mul2(du, pack2(v[2 * n], v[2 * n + 1])));
+            if constexpr (kPad) hp[n] &= (uint64_t)keep(2 * n) | (uint64_t)keep(2 * n + 1) << 32;
             if constexpr (kY) {
               const uint64_t cn = pack2(v[NPL + 2 * n], v[NPL + 2 * n + 1]);
               yp = n == 0 ? mul2(hp[n], cn) : fma2(hp[n], cn, yp);
@@ -459,26 +463,26 @@ __global__ void __launch_bounds__(256) scan_carry_kernel(const ScanArgs a, int n
   }
 }
 
-template <typename T, int S, int NPL, bool WIDE>
+template <typename T, int S, int NPL, bool WIDE, bool kPad>
 cudaError_t launch_tiles(const ScanArgs& a, const ScanPlan& p, void* ws, cudaStream_t st) {
   using Sm = Smem<T, S, NPL>;
   const dim3 grid((unsigned)ceil_div(a.C, Sm::kCh), (unsigned)p.nchunk, (unsigned)a.B);
   static OncePerDevice opt_in;
   cudaError_t e = opt_in.run([] {
-    const cudaError_t r = cudaFuncSetAttribute(scan_kernel<T, S, NPL, WIDE, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * (int)sizeof(Sm));
-    return r != cudaSuccess ? r : cudaFuncSetAttribute(scan_kernel<T, S, NPL, WIDE, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * (int)sizeof(Sm));
+    const cudaError_t r = cudaFuncSetAttribute(scan_kernel<T, S, NPL, WIDE, true, kPad>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * (int)sizeof(Sm));
+    return r != cudaSuccess ? r : cudaFuncSetAttribute(scan_kernel<T, S, NPL, WIDE, false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * (int)sizeof(Sm));
   });
   if (e != cudaSuccess) return e;
   float* state = p.nchunk > 1 ? (float*)((char*)ws + p.off_state) : nullptr;
   float* sum = p.nchunk > 1 ? (float*)((char*)ws + p.off_sum) : nullptr;
   if (p.nchunk > 1) {
-    e = launch_programmatic(scan_kernel<T, S, NPL, WIDE, false>, grid, kThreads + kStagers, 2 * sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
+    e = launch_programmatic(scan_kernel<T, S, NPL, WIDE, false, false>, grid, kThreads + kStagers, 2 * sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
     if (e != cudaSuccess) return e;
     const int64_t n = (int64_t)a.B * a.C * a.Ns;
     e = launch_programmatic(scan_carry_kernel, dim3((unsigned)((n + 255) / 256)), 256, 0, st, a, p.nchunk, state, (const float*)sum);
     if (e != cudaSuccess) return e;
   }
-  return launch_programmatic(scan_kernel<T, S, NPL, WIDE, true>, grid, kThreads + kStagers, 2 * sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
+  return launch_programmatic(scan_kernel<T, S, NPL, WIDE, true, kPad>, grid, kThreads + kStagers, 2 * sizeof(Sm), st, a, p.chunk, p.nchunk, state, sum);
 }
 
 template <typename T, int S, int NPL>
@@ -486,7 +490,8 @@ cudaError_t launch_states(const ScanArgs& a, const ScanPlan& p, void* ws, cudaSt
   const size_t e = sizeof(T);
   const bool wide = ((uintptr_t)a.u | (uintptr_t)a.dt | (uintptr_t)a.z | (uintptr_t)a.y | a.C * e | a.us.tok * e | a.us.batch * e |
                      a.ds.tok * e | a.ds.batch * e | (a.z ? (a.zs.tok | a.zs.batch) * e : 0)) % 16 == 0;
-  return wide ? launch_tiles<T, S, NPL, true>(a, p, ws, st) : launch_tiles<T, S, NPL, false>(a, p, ws, st);
+  if (a.Ns < S * NPL) return wide ? launch_tiles<T, S, NPL, true, true>(a, p, ws, st) : launch_tiles<T, S, NPL, false, true>(a, p, ws, st);
+  return wide ? launch_tiles<T, S, NPL, true, false>(a, p, ws, st) : launch_tiles<T, S, NPL, false, false>(a, p, ws, st);
 }
 
 template <typename T>

@@ -255,6 +255,30 @@ def test_steps_of_nothing_leave_the_state_for_any_A(B, L, C, Ns, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("Ns", [1, 3, 4, 5, 17, 33, 40])
+@pytest.mark.parametrize("B,L,C", [(1, 3, 64), (2, 90, 2048), (1, 700, 64), (3, 60, 5000)])
+def test_infinities_with_fewer_states_than_lanes_hold(B, L, C, Ns, dtype):
+    """All of a channel's own terms plus infinity: so are its results from there on, whatever number of states lanes are left without.
+    Single tokens, one pass on eight lanes and on four, chunks."""
+    i = _scan_inputs(B, L, C, Ns, dtype)
+    for name in ("Bm", "Cm", "z", "D", "state"):
+        i[name] = i[name].abs() + 0.1
+    i["A"] = torch.full_like(i["A"], -0.01)
+    at = L // 2
+    for name in ("u", "dt"):
+        j = dict(i, **{name: i[name].abs()})
+        j[name][:, at, 3] = math.inf
+        if name == "dt":
+            j["u"], j["A"] = i["u"].abs() + 0.1, torch.full_like(i["A"], 0.01)   # (a step of infinity: the state too grows beyond all)
+        clean = jv.selective_scan(**dict(j, **{name: i[name].abs()}))
+        h = torch.empty_like(i["state"])
+        y = jv.selective_scan(**j, state_out=h)
+        assert (y[:, at:, 3] == math.inf).all() and (h[:, 3] == math.inf).all()
+        assert torch.equal(y[:, :at], clean[:, :at]) and torch.equal(y[:, :, 4:], clean[:, :, 4:]) and torch.isfinite(y[:, :, :3]).all()
+
+
+@pytest.mark.gpu
 def test_results_on_another_stream_do_not_lie_where_earlier_work_still_writes():
     i = _scan_inputs(1, 1000, 256, 16, torch.float32)
     w = torch.randn(256, 4, device="cuda")
