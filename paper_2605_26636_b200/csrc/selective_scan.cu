@@ -444,6 +444,14 @@ __global__ void __launch_bounds__(kThreads + kStagers, S == 4 && NPL <= 4 ? 2 : 
   }
 }
 
+// h after steps of sum: exp(A sum) h, x = sum * A2.  Far powers in three parts: one that leaves fp32 may take h, or what is left of it, back
+// into it, as the steps one by one do.  No state stays none, whatever it is multiplied with.
+__device__ __forceinline__ float carried(float h, float x) {
+  if (fabsf(x) <= 120.f) return ex2(x) * h;
+  const float f = ex2(x * (1.f / 3.f));
+  return h == 0.f ? 0.f : h * f * f * f;
+}
+
 // State from chunk to chunk, in place: a chunk's own state out, the state that it begins with in
 __global__ void __launch_bounds__(256) scan_carry_kernel(const ScanArgs a, int nchunk, float* ws_state, const float* ws_sum) {
   griddep_wait();
@@ -459,7 +467,7 @@ __global__ void __launch_bounds__(256) scan_carry_kernel(const ScanArgs a, int n
     float* st = ws_state + ((int64_t)b * nchunk + k) * per + e;
     const float own = *st, sum = ws_sum[((int64_t)b * nchunk + k) * a.C + c];
     *st = h;
-    h = fmaf(ex2(sum * A2), h, own);
+    h = carried(h, sum * A2) + own;
   }
 }
 

@@ -279,6 +279,28 @@ def test_infinities_with_fewer_states_than_lanes_hold(B, L, C, Ns, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("step,start", [(-3.0, 1e-33), (-40.0, 0.0), (3.0, 1e33)])
+def test_chunks_whose_steps_together_leave_fp32(step, start):
+    """Steps of the first 32 tokens (a chunk's) that multiply the state by e^96 or e^-96 together: as one by one, a state that is back
+    within fp32 is kept, and none stays none."""
+    L, C, Ns = 1000, 64, 16
+    i = _scan_inputs(1, L, C, Ns, torch.float32)
+    i.update(A=torch.full((C, Ns), -1.0, device="cuda"), u=torch.zeros(1, L, C, device="cuda"), dt=torch.zeros(1, L, C, device="cuda"),
+             dt_bias=None, state=torch.full((1, C, Ns), start, device="cuda"))
+    i["dt"][:, :32] = step
+    if start == 0.0:
+        i["u"][:, 500:], i["dt"][:, 500:] = 1.0, 0.01
+    assert jv.lib().jv_selective_scan_workspace_bytes(ctypes.byref(jv.JvScanShape(1, L, C, Ns, jv.JV_F32, 0))) > 0     # in chunks
+    h = torch.empty_like(i["state"])
+    y = jv.selective_scan(**i, softplus=False, state_out=h)
+    assert torch.isfinite(y).all()
+    _, _, want, bound = _scan_reference(i, [L], softplus=False)
+    # beside what the recurrence carries along: the three factors, 2^-22 and the rounding of a third of 139 binary orders each, two products
+    bound = bound + (3 * (2.0 ** -22 + 47 * U) + 4 * U) * want.abs()
+    assert ((h.double() - want).abs() <= bound).all() and (h != 0).all()
+
+
+@pytest.mark.gpu
 def test_results_on_another_stream_do_not_lie_where_earlier_work_still_writes():
     i = _scan_inputs(1, 1000, 256, 16, torch.float32)
     w = torch.randn(256, 4, device="cuda")
