@@ -308,8 +308,9 @@ jv_status jv_layer_norm_grad(const void* dy, const void* x, const float* w, cons
  *           finite values of v do not reach it; infinities and NaN among the rows of v below kv_len may (0 times infinity).
  * All rows of o are written.  A query that sees no key gets zeros.  As everywhere in this library a key of score -inf weighs
  * nothing, a row that sees keys but none of weight is NaN, and a score of +inf or NaN makes its row NaN.
- * bf16 tensors with D = 64: tensor cores, fp32 softmax and sums; P rounded to bf16, in map 0 (which weighs most) partly or wholly as two
- * bf16 terms; one rounding of o.  Tiles of queries take exponentials against the largest score of 64 of a row's keys; a row whose later
+ * bf16 tensors with D = 64: tensor cores, fp32 softmax and sums, one rounding of o.  Few queries (H / Hkv * Nq <= 16) take P as two bf16
+ * terms (off by 2^-16 of itself at most); more of them P rounded to bf16 (2^-8), but as two terms the first 32 of every 64 keys of map 0, the
+ * one that weighs most.  Tiles of queries take exponentials against the largest score of 64 of a row's keys; a row whose later
  * scores lie 41 or more above it, or whose sums leave the range of fp32, is computed again in fp32 within the call: exact,
  * but slow where many rows are so.  Such calls obey the status word (Errors above).  f32, and bf16 with other D <= 64: fp32 arithmetic,
  * one warp per row (rows of multiples of 16 bytes).  scale <= 0 selects 1/sqrt(D).

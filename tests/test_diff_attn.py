@@ -294,6 +294,70 @@ def test_norms_of_rows_whose_squares_leave_fp32(H, Nq, Nk, dtype, D, size, eps):
     _check(q, k, (v.float() * size).to(dtype), lam, w, eps=eps, rms=False)
 
 
+def _cancelling(H, Nq, Nk, which, half, device):
+    """Inputs whose result hangs on the last bits of the probabilities of map ``which``: scores that are exact in 32 bits (one product of
+    powers of 2 and values of 6 bits), values of neighbouring keys that cancel but for a difference of their scores of 1/32.  Keys of
+    the other map weigh alike, so that its result is nothing.  half: only the first 32 of every 64 keys weigh anything."""
+    g = torch.Generator().manual_seed(Nk + Nq)
+    q, k = torch.zeros(1, H // 2, 2, Nq, 64), torch.zeros(1, H // 2, 2, Nk, 64)
+    q[:, :, which, :, 0] = 2.0 ** -torch.randint(0, 3, (1, H // 2, Nq), generator=g).float()
+    k0 = torch.randint(-32, 32, (1, H // 2, Nk // 2), generator=g) / 32
+    k[:, :, which, :, 0] = torch.stack((k0, k0 + torch.randint(0, 2, k0.shape, generator=g) / 16 - 1 / 32), -1).flatten(2)
+    q[..., 1] = 1.0
+    if half:
+        k[..., torch.arange(Nk) % 64 >= 32, 1] = -200.0           # exp(-200): nothing in 32 bits
+    v0 = torch.randn(1, H, Nk // 2, 64, generator=g).to(torch.bfloat16)
+    v = torch.stack((v0, -v0), 3).flatten(2, 3)
+    return [t.reshape(1, H, -1, 64).to(torch.bfloat16).to(device) for t in (q, k, v)]
+
+
+def _cancelling_reference(q, k, v):
+    """The result for lambda = 1 (x = P0 v - P1 v) in 64 bits, and what the arithmetic may add to its rounding: a probability's two
+    terms 2^-16 of it; its exponential and argument (4 at most) 2^-22 and 8 U, the sum of 256 of them 256 U, its products' 32 U and
+    partial sums: below 2^-14 together."""
+    o, bound = _reference(q, k, v, torch.zeros(4, 64, device=q.device), 1.0, None, 0.0, False, None, None, 1.0)
+    single = 1.1 * (2.0 ** -8 + 2.0 ** -12)                          # (what _reference grants a probability, of both maps)
+    return o, bound / single * 2.0 ** -14
+
+
+CANCELLING = [(2, 1, 256, 0, False), (2, 1, 256, 1, False), (4, 7, 200, 0, False), (4, 16, 130, 1, False), (12, 3, 64, 1, False),     # rows
+              (2, 128, 256, 0, True), (4, 200, 128, 0, True), (300, 33, 64, 0, True)]                                                # tiles
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H,Nq,Nk,which,half", CANCELLING)
+def test_second_terms_of_the_probabilities(H, Nq, Nk, which, half):
+    """Few queries have them for all keys of both maps, tiles of queries for the first 32 of every 64 keys of map 0."""
+    q, k, v = _cancelling(H, Nq, Nk, which, half, "cuda")
+    ref, bound = _cancelling_reference(q, k, v)
+    o = jv.diff_attn(q, k, v, torch.zeros(4, 64, device="cuda"), 1.0, scale=1.0)
+    assert ((o.double() - ref).abs() <= 2.0 ** -8 * (ref.abs() + bound) + bound).all()
+
+
+@pytest.mark.parametrize("H,Nq,Nk,which,half", [c for c in CANCELLING if c[0] < 100])
+def test_second_terms_decide_that_comparison(H, Nq, Nk, which, half):
+    """Probabilities in 64 bits rounded as the kernels round them: with both terms within the bound; with one, or with the second at
+    another key's values, a good part of the results is not."""
+    q, k, v = _cancelling(H, Nq, Nk, which, half, "cpu")
+    ref, bound = _cancelling_reference(q, k, v)
+    s = q.double().reshape(1, H // 2, 2, Nq, 64) @ k.double().reshape(1, H // 2, 2, Nk, 64).transpose(3, 4)
+    vv = v.double().reshape(1, H // 2, 2, Nk, 64).transpose(2, 3).reshape(1, H // 2, 1, Nk, 128)
+    p = (s - s.amax(-1, keepdim=True)).exp()
+    hi = p.to(torch.bfloat16).double()
+    lo = (p - hi).to(torch.bfloat16).double()
+
+    def share(x):
+        x = x[:, :, 0] - x[:, :, 1]
+        o = x.reshape(1, H // 2, Nq, 2, 64).transpose(2, 3).reshape(1, H, Nq, 64)
+        o = o.to(torch.bfloat16).double()
+        return float(((o - ref).abs() > 2.0 ** -8 * (ref.abs() + bound) + bound).double().mean())
+
+    total = p.sum(-1, keepdim=True)
+    assert share((hi @ vv + lo @ vv) / total) == 0
+    assert share(hi @ vv / total) > 0.2
+    assert share((hi @ vv + lo @ vv.roll(8, 3)) / total) > 0.2
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("Nq", [1, 130])
 def test_calls_while_the_status_word_is_set(Nq):
