@@ -207,6 +207,31 @@ def test_lanes_and_chunks(B, L, C, Ns):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("Ns", [5, 8, 16, 32, 40])
+@pytest.mark.parametrize("B,L,off", [(2, 90, 0), (5, 300, 0), (2, 90, -3), (2, 90, -8)])
+def test_eight_lanes_in_one_pass(B, L, off, Ns, dtype):
+    """Channels that fill two thirds of the SMs in blocks of 32, not in blocks of 64; whole blocks and a remainder, on 16-byte boundaries and
+    off them; lengths, and the state in its own place."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    C = 32 * -(-5 * sms // (6 * B)) + off                                    # a quarter more blocks of 32 than that takes
+    blocks = lambda n: B * -(-C // n)
+    assert 3 * blocks(64) < 2 * sms <= 3 * blocks(32)
+    for softplus in (0, 1):
+        shape = jv.JvScanShape(B, L, C, Ns, jv.JV_BF16 if dtype is torch.bfloat16 else jv.JV_F32, softplus)
+        assert jv.lib().jv_selective_scan_workspace_bytes(ctypes.byref(shape)) == 0        # one pass
+    i = _scan_inputs(B, L, C, Ns, dtype)
+    _scan_check(i, dtype)
+    lens = torch.tensor([L - 31 * b for b in range(B)], dtype=torch.int32, device="cuda")
+    _scan_check(dict(i, D=None), dtype, lens)
+    want, h, run = torch.full((B, L, C), CANARY, dtype=dtype, device="cuda"), torch.empty_like(i["state"]), i["state"].clone()
+    got = want.clone()
+    jv.selective_scan(**i, lens=lens, out=want, state_out=h)
+    jv.selective_scan(**dict(i, state=run), lens=lens, out=got, state_out=run)
+    assert torch.equal(got, want) and torch.equal(run, h)
+
+
+@pytest.mark.gpu
 def test_far_values_and_no_numbers():
     i = _scan_inputs(1, 40, 64, 16, torch.float32)
     big = dict(i, dt=torch.where(torch.rand_like(i["dt"]) < 0.1, 60.0, -90.0))     # steps of 60 (the state forgets all) and of nothing
