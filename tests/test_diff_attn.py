@@ -461,6 +461,21 @@ def test_refusals(L):
         assert _call(L, w=None, eps=-1.0, kv_len=LEN) in (jv.JV_ERR_CUDA, jv.JV_ERR_UNSUPPORTED)
 
 
+@pytest.mark.parametrize("Nq", [8, 9, 300])
+def test_workspace_refusals(L, Nq):
+    """Of the few queries' plan (16 rows on a pair of keys) and of the tiles'."""
+    shp = _shape(Nq=Nq, Nk=640)
+    need = L.jv_diff_attn_workspace_bytes(ctypes.byref(shp))
+    assert need > 0
+    for kw in (dict(ws=None), dict(ws=WS + 16), dict(n=need - 1), dict(n=0)):
+        assert _call(L, shp, **kw) == jv.JV_ERR_WORKSPACE, kw
+    for p in (Q, K, V, O, LAM, W):
+        assert _call(L, shp, ws=p) == jv.JV_ERR_INVALID_ARG
+    assert _call(L, shp, kv_len=WS + 4 * (need // 8)) == jv.JV_ERR_INVALID_ARG      # an input inside it
+    if not torch.cuda.is_available():
+        assert _call(L, shp, n=need) in (jv.JV_ERR_CUDA, jv.JV_ERR_UNSUPPORTED)
+
+
 def test_binding_refuses():
     t = torch.zeros(1, 2, 4, 64, dtype=torch.bfloat16)
     with pytest.raises(ValueError):
