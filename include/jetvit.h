@@ -306,6 +306,7 @@ jv_status jv_layer_norm_grad(const void* dy, const void* x, const float* w, cons
  *   causal  query i sees the keys j <= q_pos[b] + i only; q_pos device int32 [B] or NULL: Nk - Nq, the queries being the last of
  *           the Nk positions (0 for a whole prompt); any value is served.  A key that a query does not see weighs exactly nothing, so
  *           finite values of v do not reach it; infinities and NaN among the rows of v below kv_len may (0 times infinity).
+ * Nq and Nk are at most 2^24, and B * H / 2 * ceil(Nq / 128) * ceil(Nk / 128) at most 2^36 (some 15 minutes' work).
  * All rows of o are written.  A query that sees no key gets zeros.  As everywhere in this library a key of score -inf weighs
  * nothing, a row that sees keys but none of weight is NaN, and a score of +inf or NaN makes its row NaN.
  * bf16 tensors with D = 64: tensor cores, fp32 softmax and sums, one rounding of o.  Few queries (H / Hkv * Nq <= 16) take P as two bf16

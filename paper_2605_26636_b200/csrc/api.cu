@@ -180,6 +180,8 @@ jv_status check_diff(const jv_diff_shape* s, InStrides* qs, InStrides* ks) {
   if (s->causal != 0 && s->causal != 1) return JV_ERR_INVALID_ARG;
   if (s->H % 2 || s->Hkv % 2 || s->H % s->Hkv) return JV_ERR_INVALID_ARG;
   if (s->Nq > (1 << 24) || s->Nk > (1 << 24) || (int64_t)s->B * s->H > 65535 || s->D > 64) return JV_ERR_UNSUPPORTED;
+  // tiles of 128 queries and keys: a block counts its share of them in 32 bits
+  if ((int64_t)s->B * (s->H / 2) * ceil_div(s->Nq, 128) * ceil_div(s->Nk, 128) > (int64_t)1 << 36) return JV_ERR_UNSUPPORTED;
   const int64_t e = s->dtype == JV_F32 ? 4 : 2;
   if (s->D * e % 16) return JV_ERR_UNSUPPORTED;
   if (!diff_strides(s->q_stride, s->H, s->Nq, s->D, qs) || !diff_strides(s->kv_stride, s->Hkv, s->Nk, s->D, ks)) return JV_ERR_INVALID_ARG;

@@ -461,6 +461,15 @@ def test_refusals(L):
         assert _call(L, w=None, eps=-1.0, kv_len=LEN) in (jv.JV_ERR_CUDA, jv.JV_ERR_UNSUPPORTED)
 
 
+def test_work_that_a_block_cannot_count(L):
+    n = 1 << 24
+    for B, H, Nq, Nk, ok in ((1, 8, n, n, True), (1, 10, n, n, False), (1000, 64, n, n, False), (1000, 64, 1, n, True), (2, 64, n // 16, n, True)):
+        shp = _shape(B=B, H=H, Hkv=2, Nq=Nq, Nk=Nk)
+        assert (L.jv_diff_attn_workspace_bytes(ctypes.byref(shp)) > 0) == ok, (B, H, Nq, Nk)
+        if not ok:
+            assert _call(L, shp) == jv.JV_ERR_UNSUPPORTED
+
+
 @pytest.mark.parametrize("Nq", [8, 9, 300])
 def test_workspace_refusals(L, Nq):
     """Of the few queries' plan (16 rows on a pair of keys) and of the tiles'."""
