@@ -215,16 +215,18 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
       int n = 0;                 // items seen
       int ks = 0, vs = 0;        // ring stages of the next K and V tile
       uint32_t kpar = 1, vpar = 1;   // parity of the "empty" phase this pass over each ring waits for
-      int issued_v = 0;          // for the abort path: V copies issued so far
+      int issued_q = 0, issued_k = 0, issued_v = 0;   // for the abort path: tiles whose copies have been issued so far
       while (ok && it.next(p.items)) {
         const int hk = 2 * (it.ipair / p.share), qb = n & 1;
         ok = wait(&bar->q_empty[qb], ((n >> 1) & 1) ^ 1);
         if (!ok) break;
         load_tile(sQ + qb * kTileBytes, &mapQ, &bar->q_full[qb], it.iqt * kTile, 2 * it.ipair, it.ib);
+        ++issued_q;
         for (int j = it.t0; j < it.t1; ++j) {
           ok = wait(&bar->k_empty[ks], kpar);
           if (!ok) break;
           load_tile(sK + ks * kTileBytes, &mapK, &bar->k_full[ks], j * kTile, hk, it.ib);
+          ++issued_k;
           if (++ks == kKS) { ks = 0; kpar ^= 1; }
           ok = wait(&bar->v_empty[vs], vpar);
           if (!ok) break;
@@ -235,12 +237,15 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
         ++n;
       }
       if (!ok) {
-        // let the copies still in flight land before the CTA leaves (bounded by the same limit): those of V by their
-        // barriers, those of K and Q around them by a millisecond from here
+        // let the copies still in flight land before the CTA leaves (bounded by the same limit)
         const unsigned long long t0 = globaltimer();
-        for (int g = max(0, issued_v - kVS); g < issued_v; ++g)
-          while (!mbar_try(&bar->v_full[g % kVS], (g / kVS) & 1) && globaltimer() - t0 < kWaitLimitNs) {}
-        while (globaltimer() - t0 < 1000000ull) {}
+        auto landed = [&](uint64_t* full, int ring, int issued) {
+          for (int g = max(0, issued - ring); g < issued; ++g)
+            while (!mbar_try(&full[g % ring], (g / ring) & 1) && globaltimer() - t0 < kWaitLimitNs) {}
+        };
+        landed(bar->q_full, kQB, issued_q);
+        landed(bar->k_full, kKS, issued_k);
+        landed(bar->v_full, kVS, issued_v);
       }
     }
     __syncwarp();
