@@ -103,6 +103,33 @@ struct NormParams {
   float eps;
 };
 
+// A row whose variance is not safely within fp32 (values some 1e17 apart and more, or, without an eps, 1e-15 and less), by the threads that
+// share it, once more from the start: the row, and eps with it, times the power of two k.  A call of its own at the end of the kernel, so that
+// the rest of it keeps its registers (in its middle it took 17 % of the rows read value by value).
+template <typename T, bool BLOCK>
+__device__ __noinline__ void far_row(const T* x, const float* w, const float* b, T* y, float* mean, float* rstd, int C, float eps, float k,
+                                     float* red, int turn) {
+  const int tl = BLOCK ? threadIdx.x : threadIdx.x & 31, nl = BLOCK ? blockDim.x : 32;
+  const float inv_c = 1.f / (float)C;
+  float s[1] = {0.f};
+  for (int c = tl; c < C; c += nl) s[0] += to_f32(x[c]) * k;
+  row_sums<BLOCK, 1>(s, red, turn);
+  const float m = s[0] * inv_c;
+  s[0] = 0.f;
+  for (int c = tl; c < C; c += nl) {
+    const float d = fmaf(to_f32(x[c]), k, -m);
+    s[0] = fmaf(d, d, s[0]);
+  }
+  row_sums<BLOCK, 1>(s, red, turn);
+  const float r = rsqrtf(fmaf(s[0], inv_c, eps * k * k));
+  if (!BLOCK) __syncwarp();                         // (what is written here other threads have written before)
+  for (int c = tl; c < C; c += nl) from_f32(y + c, fmaf(fmaf(to_f32(x[c]), k, -m) * r, w ? __ldg(w + c) : 1.f, b ? __ldg(b + c) : 0.f));
+  if (mean && tl == 0) {
+    *mean = m * (k > 1.f ? 0x1p-100f : 0x1p+80f);
+    *rstd = r * k;
+  }
+}
+
 // Columns of lane `tl` (of `nl` that share a row): pieces tl, tl + nl, ...  R rows of a warp at a time: w and b pass through L1 once for
 // them (for one row of bf16 values they are four times the row's bytes).
 template <typename T, int VEC, int NCH, bool BLOCK, int R>
@@ -182,6 +209,15 @@ __global__ void __launch_bounds__(BLOCK ? 512 : 128, 1) layer_norm_kernel(const 
         p.mean[row0 + r] = mean[r];
         p.rstd[row0 + r] = rstd[r];
       }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    // variances from 1e-30 to fp32's end; beside a mean of 1 and more a smaller one is 0, no two values are that close
+    const bool tiny = rstd[r] > 1e15f;
+    if ((rstd[r] > 0.f && !tiny) || (tiny && fabsf(mean[r]) >= 1.f) || row0 + r >= p.rows) continue;
+    const int64_t row = row0 + r;
+    far_row<T, BLOCK>((const T*)p.x + row * p.x_stride, p.w, p.b, (T*)p.y + row * p.C, p.mean ? p.mean + row : nullptr,
+                      p.mean ? p.rstd + row : nullptr, p.C, p.eps, tiny ? 0x1p+100f : 0x1p-80f, red, turn);
+  }
 }
 
 // stages of a warp's ring: 1 KB for a piece of x and dy each

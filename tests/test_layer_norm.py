@@ -54,6 +54,27 @@ def test_forward(C, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("C", [7, 384, 1024, 1032, 5000])
+@pytest.mark.parametrize("size,eps", [(1e20, 1e-5), (1e30, 0.0), (1e37, 1e-5), (1e-18, 0.0), (1e-25, 1e-38)])
+def test_variances_that_leave_fp32(C, dtype, size, eps):
+    """Every other row far larger, or smaller, than its squares in fp32 allow, two rows of bf16 to a warp among them; a row of one value
+    beside them."""
+    for rows in (5, 5001):
+        x, _, w, b = _inputs(rows, C, dtype, seed=4, offset=0.0)
+        x[::2] = (x[::2].float() * size).to(dtype)
+        if eps > 0.0:
+            x[1] = 3.0
+        stats = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        y = jv.layer_norm(x, w, b, eps=eps, stats=stats)
+        ref, bound, m, r = _reference(x, w, b, eps)
+        assert ((y.double() - ref).abs() <= HALF[dtype] * (ref.abs() + bound) + bound).all()
+        assert ((stats[0].double() - m).abs() <= 64 * U * x.double().abs().mean(-1)).all()
+        # (1 / standard deviation itself is a small, or large, fp32 number: within 2^-126 it has fewer bits)
+        assert ((stats[1].double() - r).abs() <= (64 * U * r * (1 + (r * x.double().abs().mean(-1)) ** 2 * U) + 2.0 ** -149)).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("C", COLS)
 def test_gradient(C, dtype):
     for rows in (1, 6, 2500 if C <= 2048 else 700):
