@@ -274,7 +274,7 @@ jv_status jv_out_proj(const void* o, const void* w, const float* bias, void* y, 
  * wanted; with both NULL no scratch is needed.
  * rows > 0, 0 < C <= 16384, eps >= 0.  Any alignment to the element is served; where every row and vector starts on a 16-byte boundary,
  * 16 bytes at a time (faster).  Outputs share no byte with an input or each other.  Arithmetic in fp32, statistics of the centred
- * values; dw and db are summed in a fixed order (results repeat bit for bit).
+ * values, which may have any size that x can have (mean and rstd are fp32 numbers); dw and db are summed in a fixed order (results repeat bit for bit).
  * jv_layer_norm_grad_workspace_bytes() sizes ws (256-byte aligned); 0 on invalid arguments.
  */
 typedef struct {
@@ -309,12 +309,14 @@ jv_status jv_layer_norm_grad(const void* dy, const void* x, const float* w, cons
  * Nq and Nk are at most 2^24, and B * H / 2 * ceil(Nq / 128) * ceil(Nk / 128) at most 2^36 (some 15 minutes' work).
  * All rows of o are written.  A query that sees no key gets zeros.  As everywhere in this library a key of score -inf weighs
  * nothing, a row that sees keys but none of weight is NaN, and a score of +inf or NaN makes its row NaN.
+ * With norm_w the mean square may lie anywhere; eps = 0 is served (a row that sees keys whose x is all 0 is then 0 / 0).
  * bf16 tensors with D = 64: tensor cores, fp32 softmax and sums, one rounding of o.  Few queries (H / Hkv * Nq <= 16) take P as two bf16
  * terms (off by 2^-16 of itself at most); more of them P rounded to bf16 (2^-8), but as two terms the first 32 of every 64 keys of map 0, the
  * one that weighs most.  Tiles of queries take exponentials against the largest score of 64 of a row's keys; a row whose later
  * scores lie 41 or more above it, or whose sums leave the range of fp32, is computed again in fp32 within the call: exact,
- * but slow where many rows are so.  Such calls obey the status word (Errors above).  f32, and bf16 with other D <= 64: fp32 arithmetic,
- * one warp per row (rows of multiples of 16 bytes).  scale <= 0 selects 1/sqrt(D).
+ * but slow where many rows are so (one warp a row: two causal prompts of 4096 tokens and 8 pairs, 60 ms instead of 0.13 if all are).  Such
+ * calls obey the status word (Errors above).  f32, and bf16 with other D <= 64: fp32 arithmetic, one warp per row (rows of multiples of 16
+ * bytes); right but slow, 50 ms for those prompts.  scale <= 0 selects 1/sqrt(D).
  * Few queries (single tokens against a cache) and prompts take different kernels; both spread the keys over the whole GPU whatever
  * the lengths are.  ws must cover jv_diff_attn_workspace_bytes() (0 on invalid arguments), 256-byte aligned.
  */
@@ -338,6 +340,9 @@ jv_status jv_diff_attn(const void* q, const void* k, const void* v, void* o, con
                        float scale, void* ws, size_t ws_bytes, void* cuda_stream);
 
 /*
+ * The two calls of a state-space mixer work on token rows [B, L, C], the layout that jv_layer_norm takes and the input rows of
+ * jv_qkv_proj have; they are no mixer of jv_hybrid_mixers' schedule, whose arrays are [B, H, N, D].
+ *
  * The short causal convolution of a state-space mixer, one filter per channel over a token and the K - 1 before it:
  *   u[b, t, c] = act(bias[c] + sum_(j < K) w[c, j] x[b, t - (K - 1) + j, c]),  act(x) = x / (1 + exp(-x)) with silu = 1, x with 0
  * x is [B, L, C] with x_stride elements between {token rows, batch elements} (0: C; L rows), u [B, L, C] contiguous,

@@ -11,14 +11,17 @@
 // state.
 //
 // The softmax has no running maximum.  The two sets of a map add to one accumulator, so all their exponentials are against one reference
-// a row: the maximum of the item's first 64 keys.  A later score may lie far above it: probabilities, sums and accumulators are
-// floating point with 8 bits of exponent, and as precise at 2^60 as at 1.  A row whose sum leaves [2^-60, 2^60], or whose result
-// is not finite, is marked, and done again by the second launch, exactly and slowly, from the inputs (so are infinities and NaN among
-// them).  That takes a score 41 above, or below, every one of the first 64 keys; it saves the maximum of every other
+// a row: the maximum of the first 64 keys of the item, or of the block's part of it.  A later score may lie far above it: probabilities,
+// sums and accumulators are floating point with 8 bits of exponent, and as precise at 2^60 as at 1.  A row whose sum leaves
+// [2^-60, 2^60] in some part, whose result is not finite, or whose mean square is not safely within fp32, is marked, and done again by
+// the second launch, exactly and slowly, from the inputs (so are infinities and NaN among them).  That takes a score 41 above every one of
+// those 64 keys (or, where none of them weighs anything, 41 off zero).  A call all of whose rows are so takes 60 ms where it takes 0.13 (two
+// causal prompts of 4096 tokens, 8 pairs).  It saves the maximum of every other
 // step, and its order between the sets: half of a step's instructions.  The exponentials are all the MUFU unit's: it gives 0 for a key
 // that scores -inf, and two of eight by a polynomial are no faster (B = 4, 8 pairs, 73 x 73 tokens, without second terms: 651 us, 661).
 //
-// What bounds a step is the chain of the warps that issue for it: beside four busy softmax warps in its sub-core an instruction takes such a
+// What bounds a step is the latency between its roles (MUFU unit 59 %, issue slots 54 %, tensor pipe 51 % of two causal prompts of 4096
+// tokens), first the chain of the warps that issue for it: beside four busy softmax warps in its sub-core an instruction takes such a
 // warp some 8 clocks, a look at a barrier 110 and more.  Scores and products from one warp per map, each phase elected and
 // voted on by the whole warp, cost it 1300 clocks a step, whatever was left out of the arithmetic.  So one lane per role, three
 // issuers, and the softmax warps' looks at their barriers ahead of the arithmetic that hides them.
@@ -32,7 +35,7 @@
 // attn_diff.cuh) go to the workspace as they are.
 //
 // Measured, with the launch that merges: B = 4, 8 pairs, 73 x 73 tokens 735 us (850 at the power cap; 698 GF: 950 TF), two causal prompts
-// of 4096 tokens, 8 pairs, 127 us, 256 queries against 16384 keys, 8 pairs, 48 us.
+// of 4096 tokens, 8 pairs, 127 to 143 us by the board, 256 queries against 16384 keys, 8 pairs, 48 us.
 //
 // Keys that a row does not see are set to -inf behind the load of the scores; rows of V that lie behind a length may hold anything, and
 // are overwritten with zeros in shared memory before the first product of their tile.
@@ -77,7 +80,7 @@ struct __align__(8) Barriers {
   volatile uint32_t abort_flag;
   int redo;
 };
-constexpr size_t kSmemTiles = (kQB + kKS + kVS) * (size_t)kTileBytes;          // 224 KB
+constexpr size_t kSmemTiles = (kQB + kKS + kVS) * (size_t)kTileBytes;          // 192 KB
 constexpr size_t kSmemLo = 2 * (size_t)kLoBytes;                               // the two sets of map 0
 constexpr size_t kSmemBytes = kSmemTiles + kSmemLo + sizeof(Barriers) + 1024;  // + alignment slack
 static_assert(kSmemBytes <= 227 * 1024, "shared memory of one block");
@@ -545,7 +548,7 @@ attn_diff_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant
 // Blocks of a call, one per SM at most: one for every item, or for every kTilesMin tiles of the longest that the items can be
 constexpr int kTilesMin = 4;
 // An item costs as much as four tiles beside its own (first scores, epilogue).  Measured, in units of 1 / 2 / 3 / 4 / 6 tiles: two
-// causal prompts of 4096 tokens, 8 pairs, 173 / 137 / 127 / 127 / 132 us; 73 x 73 tokens 744 to 784 either way.
+// causal prompts of 4096 tokens, 8 pairs, on one board 173 / 137 / 127 / 127 / 132 us; 73 x 73 tokens 744 to 784 either way.
 constexpr int kLead = 4, kWhole = 2;
 int diff_blocks(int B, int pairs, int Nq, int Nk) {
   const int64_t items = (int64_t)B * pairs * ceil_div(Nq, kTile), tiles = items * ceil_div(Nk, kTile);

@@ -1,5 +1,9 @@
 // Differential attention for what has no kernel of its own: f32 tensors, and bf16 ones with D other than 64.  One warp per query row and
 // pair, fp32 arithmetic (diff_row in attn_diff.cuh).
+//
+// It is right, not fast: no row shares a key with another in registers or shared memory and no row's keys are split, so latency bounds
+// it.  f32, D = 64, 8 pairs: 64 queries against 64 keys 85 us, two causal prompts of 4096 tokens 50 ms, single tokens of 32 sequences of up
+// to 16384 keys, two pairs of keys, 39 ms.
 #include "attn_diff.cuh"
 
 namespace jv {

@@ -1,7 +1,9 @@
 // The short causal convolution of a state-space mixer: every channel on its own, over the token and the K - 1 before it.
 //   u_t = act(b + sum_j w_j x_(t - K + 1 + j)),  act = x / (1 + exp(-x)) or nothing;   state: the last K - 1 inputs
 //
-// Bound by HBM: x is read once and u written once.  A thread owns 16 bytes of channels and a run of tokens, which it walks with
+// x is read once and u written once; what bounds it is not HBM yet but instructions and latency (half of the issue slots: every token
+// moves the past ones on by a register each; four loads of a thread in flight).  2 x 4096 tokens of 2048 channels 24 us in bf16 (its
+// bytes: 10.2), 26.6 in fp32 (20.5).  A thread owns 16 bytes of channels and a run of tokens, which it walks with
 // the last K - 1 inputs in registers; neighbouring threads own neighbouring channels.  The K - 1 inputs ahead of a run
 // come from the run before (L2 has them), those ahead of the first from the state.  The new state is written by the thread of the
 // first run, the only one that reads the old one: both may be the same memory.

@@ -7,6 +7,10 @@
 // (up to 32 values a lane, in 16-byte pieces 32 lanes side by side), a longer one to a block; sums are fp32, the variance is
 // that of the centred values (no cancellation where a row's mean is large against its spread).
 //
+// Measured: 32768 rows of 1024 bf16 values 22.7 us (gradient 39.6), 21845 of 1536 31.0 (150), 16384 of 2048 29.5 (131); floors 20.5 (30.7).
+// The gradient of rows longer than 1024 waits for each row where it needs it, at two blocks of few warps per SM; so it does for rows read
+// value by value (32768 of 1023: 198 us, forward 52.7).
+//
 // The gradient's blocks are persistent: every lane keeps the sums of its columns for dw and db in registers over the rows that its
 // warp walks, the warps of a block add theirs through shared memory, the blocks' partials go to the workspace and a second
 // launch adds them up, all in a fixed order: no atomics, results repeat bit for bit.
@@ -275,7 +279,7 @@ __global__ void __launch_bounds__(kGradWarps * 32, 1) layer_norm_grad_rows_kerne
   const float inv_c = 1.f / (float)p.C;
   int stage = 0;
   // a row's statistics are loaded a row ahead, too (where they were needed at once every warp waited for them, row after row: 32768 rows
-  // of 1024 bf16 values 46.9 us, now 40.0; 21316 of 768 fp32 36.0, now 34.6)
+  // of 1024 bf16 values 46.9 us, now 40.0; 21316 of 768 fp32 34 to 36 us either way)
   float mean_next = 0.f, rstd_next = 0.f;
   auto statistics = [&](int64_t row) {
     if (row < p.rows) {

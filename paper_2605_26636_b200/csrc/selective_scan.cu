@@ -534,8 +534,9 @@ ScanPlan scan_plan(int B, int L, int C, int Ns) {
   // Four lanes a channel where the channels give two of three SMs a block all the same, eight where they do with half as many
   // channels a block (and above 32 states, which eight lanes hold); chunks, which walk the exponentials twice, for two blocks an SM elsewhere
   const int64_t sms = device_sm_count(), four = (int64_t)B * ceil_div(C, kThreads / 4), eight = (int64_t)B * ceil_div(C, kThreads / 8);
-  // (Measured: 2 x 4096 tokens of 2048 channels, four lanes 308 us, eight 180; 4 x 2048 163 / 181; 1 x 4096, chunks of four / eight lanes
-  // 124 / 155.)
+  // (Measured: 2 x 4096 tokens of 2048 channels, four lanes 308 us, eight 184, chunks 255; 4 x 2048, four / eight 163 / 181; 1 x 4096, chunks
+  // of four / eight lanes 124 / 155.  Eight lanes against chunks: 2 x 4096 tokens of 1600 channels, just above two thirds of the SMs,
+  // 185 / 209; 5 x 1369 of 768, fp32, 67 / 94.  Blocks cannot know the lengths, so a ragged call takes as long as its longest sequence.)
   const bool pass = 3 * four >= 2 * sms || 3 * eight >= 2 * sms;
   p.lanes = Ns > 32 || (pass && 3 * four < 2 * sms) ? 8 : 4;
   if (!pass) {
