@@ -9,7 +9,7 @@
 // equal shares of all items' keys, so sequences of any lengths keep all SMs busy to the end).
 //
 // What bounds it: HBM, and what a call costs beside it.  32 sequences of up to 16384 keys, two pairs of keys, four pairs of queries to
-// each: 77 to 83 us by the board, with the launch that merges, for 336 MB (51 us at the rate of a copy); 67.5 us where the warps only
+// each: 77 to 86 us by the board, with the launch that merges, for 336 MB (51 us at the rate of a copy); 67.5 us where the warps only
 // take boxes in.  With eight warps for both maps, 168 registers a thread, 75.3 us where these sixteen took 74.3 (second terms in
 // map 0 alone).  Second terms of both maps' probabilities in place of map 0's alone, on one board: 81.4 -> 82.9 us, o at 1.67e-3 of the
 // exact result instead of 2.14e-3.
